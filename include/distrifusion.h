@@ -245,6 +245,71 @@ int df_cross_attn_packed(const void* xp, const void* wq_packed, const float* ln_
                          const void* text_kv_packed, void* out_packed, int B, int rows_per_batch, int C, int text_len,
                          int count, int block, float scale, void* stream);
 
+/* ---- operators of a transformer block on a patch ----------------------------------------- */
+
+/*
+ * Queries and keys of a patch's tokens, normalised per head and rotated by position in one pass (Section 4, Sparse operations: work per token
+ * runs on the fresh tokens alone).
+ *   q [B, T, heads, d], k [B, T, kv_heads, d]: a token's heads lie side by side, tokens are *_ld and batch items *_bs elements apart (slices of a
+ *     fused projection; q_out and k_out likewise, so keys can go straight into the patch's rows of a stale buffer).  k and k_out may both be
+ *     NULL (then kv_heads is 0).  An output may be its own input (same pointer, same strides); otherwise they must not overlap.
+ *   norm != 0: y = x / sqrt(mean(x^2) + eps) * gamma over the d values of a head; gamma [d] float, NULL: 1.
+ *   rot [rot_len, rot_dim / 2, 2] float, cosine and sine; NULL: no rotation (one of norm and rot must be there).  Token t of a batch item turns
+ *     by row t, or with pos [B, T] by row pos: a negative one is not rotated, one of rot_len or more gives NaN.
+ *     Pair i of the first rot_dim values of a head is (2 i, 2 i + 1) if interleaved, else (i, i + rot_dim / 2):
+ *     (a, b) -> (a cos - b sin, b cos + a sin).
+ * d % 8 == 0, d <= 256; rot_dim % 8 == 0.  Addresses and strides: multiples of 16 bytes (float), 8 bytes (bf16; fastest with 16); gamma and rot
+ * 16-byte aligned.  Sums are float: a row of values above 1e19 gives NaN.
+ */
+int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, void* q_out,
+                    long long qo_ld, long long qo_bs, void* k_out, long long ko_ld, long long ko_bs, const float* q_gamma,
+                    const float* k_gamma, const float* rot, const int* pos, int B, int T, int heads, int kv_heads, int d,
+                    int rot_dim, int rot_len, int norm, float eps, int interleaved, int dtype, void* stream);
+
+/*
+ * Keys and values of the whole image held in 4 bits between the steps (Section 4: the stale buffers of self-attention; 34 instead of 128 bytes for
+ * 64 values).  Each row (token, head) of d values is held as the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times a scale (of two equally near
+ * ones 0, 1, 2 or 4), with sign; the scale is a sixth of the row's largest magnitude, rounded to six significant bits, so that what is held is
+ * exact in bf16.  A row with an infinity or NaN is NaN as a whole, one below 2^-100 is zero.
+ *   cache  device memory of df_kv4_bytes(B, L, kv_heads, d), 16-byte aligned, d 64 or 128 (0 for sizes it does not take); rows must be
+ *          written before they are read, zeroed memory holds zeros.
+ *   df_kv4_refresh  the rows of patch `patch_idx` of N of an H x W grid of tokens (L = H * W; split as in the *_axis functions) receive
+ *          k, v [B, L / N, kv_heads, d], strides as above (16-byte multiples); one token of a sequence is patch t of N = L.  Other rows keep
+ *          what they hold.  Two neighbouring tokens share bytes: refreshes of one cache must not overlap in time.
+ *   df_kv4_read     k, v [B, L, kv_heads, d], contiguous: what all rows stand for.
+ */
+size_t df_kv4_bytes(int B, int L, int kv_heads, int d);
+int df_kv4_refresh(void* cache, const void* k, long long k_ld, long long k_bs, const void* v, long long v_ld, long long v_bs, int B,
+                   int H, int W, int kv_heads, int d, int patch_idx, int N, int dtype, int split_axis, void* stream);
+int df_kv4_read(const void* cache, void* k, void* v, int B, int L, int kv_heads, int d, int dtype, void* stream);
+
+/*
+ * Attention over a 4-bit cache, and to an encoder's states.  out [B, Lq, heads, d] (contiguous) = softmax(q k^T * scale) v per head; heads
+ * is a multiple of kv_heads, and heads h of a group share key head h / (heads / kv_heads).  q and other rows: strides as above, in multiples of
+ * 16 bytes.  scale positive and finite.  A query without any key gives zeros.  bf16 rounds the weights of the keys to bf16 for the matrix
+ * instructions; everything else is float.
+ *   df_attn_kv4            all keys from the cache: its L rows, or the first lens[b] of batch item b (device memory, NULL: L; clamped to
+ *                          0 .. L; what the other rows hold does not matter).
+ *   df_attn_displaced_kv4  df_attn_displaced_axis with the stale rows in a cache: Lq = L / N queries, the patch's own rows from
+ *                          k_fresh, v_fresh [B, L / N, kv_heads, d].
+ *   df_cross_attn          k, v [B, Lk, kv_heads, d] of another length; d % 8 == 0, d <= 128.  key_mask [B, Lk]: 0 is no key; lens as above;
+ *                          both may be NULL.  What k and v hold where there is no key does not matter, not even NaN.
+ * Workspace: df_*_workspace_bytes of the same sizes (0: none needed, NULL will do, or sizes that are not taken), 256-byte aligned, the
+ * caller's until the call's work is done; calls that overlap need workspaces of their own.  DF_ENOMEM if it is smaller.  Equal calls give
+ * equal bits.
+ */
+size_t df_attn_kv4_workspace_bytes(int B, int Lq, int L, int heads, int kv_heads, int d, int dtype);
+int df_attn_kv4(const void* q, long long q_ld, long long q_bs, const void* cache, const int* lens, void* out, int B, int Lq, int L, int heads,
+                int kv_heads, int d, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t df_attn_displaced_kv4_workspace_bytes(int B, int H, int W, int heads, int kv_heads, int d, int N, int dtype);
+int df_attn_displaced_kv4(const void* q, long long q_ld, long long q_bs, const void* k_fresh, long long k_ld, long long k_bs, const void* v_fresh,
+                          long long v_ld, long long v_bs, const void* cache, void* out, int B, int H, int W, int heads, int kv_heads, int d,
+                          int patch_idx, int N, float scale, int dtype, int split_axis, void* workspace, size_t workspace_bytes, void* stream);
+size_t df_cross_attn_workspace_bytes(int B, int Lq, int Lk, int heads, int kv_heads, int d, int masked, int dtype);
+int df_cross_attn(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, const void* v, long long v_ld,
+                  long long v_bs, const unsigned char* key_mask, const int* lens, void* out, int B, int Lq, int Lk, int heads, int kv_heads,
+                  int d, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- whole UNet step --------------------------------------------------------------------- */
 
 typedef struct df_unet_cfg {

@@ -76,6 +76,20 @@ def lib():
     L.df_pack_text_kv.argtypes = [vp, vp, i, i, i, i, vp]
     L.df_text_kv.argtypes = [vp, vp, vp, i, i, i, i, i, vp]
     L.df_cross_attn_packed.argtypes = [vp, vp, vp, vp, f, vp, vp, i, i, i, i, i, i, f, vp]
+    L.df_qk_norm_rope.argtypes = [vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, vp, vp, i, i, i, i, i, i, i, i, f, i, i, vp]
+    L.df_kv4_bytes.argtypes = [i, i, i, i]
+    L.df_kv4_refresh.argtypes = [vp, vp, ll, ll, vp, ll, ll, i, i, i, i, i, i, i, i, i, vp]
+    L.df_kv4_read.argtypes = [vp, vp, vp, i, i, i, i, i, vp]
+    L.df_attn_kv4.argtypes = [vp, ll, ll, vp, vp, vp, i, i, i, i, i, i, f, i, vp, sz, vp]
+    L.df_attn_kv4_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+    L.df_attn_displaced_kv4.argtypes = [vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, i, i, i, i, i, i, i, i, f, i, i, vp, sz, vp]
+    L.df_attn_displaced_kv4_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+    L.df_cross_attn.argtypes = [vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, vp, i, i, i, i, i, i, f, i, vp, sz, vp]
+    L.df_cross_attn_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+    for name in ("df_kv4_bytes", "df_attn_kv4_workspace_bytes", "df_attn_displaced_kv4_workspace_bytes", "df_cross_attn_workspace_bytes"):
+        getattr(L, name).restype = sz
+    for name in ("df_qk_norm_rope", "df_kv4_refresh", "df_kv4_read", "df_attn_kv4", "df_attn_displaced_kv4", "df_cross_attn"):
+        getattr(L, name).restype = i
     L.df_packed_bytes.restype = sz
     L.df_packed_bytes.argtypes = [ll, ll]
     L.df_pack_rows.argtypes = [vp, vp, i, i, vp]
@@ -170,7 +184,8 @@ def _native():
             raise DfError(f"{_HERE}/_binding.so is not built: run `python -c 'import __graft_entry__ as g; g.build()'` first") from e
         _binding.setup(DfError, torch.OutOfMemoryError, torch.AcceleratorError, *(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
             "df_strerror", "df_groupnorm_stale", "df_conv3x3_halo_axis", "df_attn_displaced", "df_attn_displaced_axis", "df_linear",
-            "df_buffer_refresh")))
+            "df_buffer_refresh", "df_qk_norm_rope", "df_kv4_bytes", "df_kv4_refresh", "df_kv4_read", "df_attn_kv4", "df_attn_kv4_workspace_bytes",
+            "df_attn_displaced_kv4", "df_attn_displaced_kv4_workspace_bytes", "df_cross_attn", "df_cross_attn_workspace_bytes")))
         _ops = _binding
     return _ops
 
@@ -280,6 +295,62 @@ def cross_attn_packed(xp, wq_packed, ln_s, ln_t, text_kv_packed, B, rows_per_bat
     _check(lib().df_cross_attn_packed(_ptr(xp), _ptr(wq_packed), _ptr(ln_s), _ptr(ln_t), ln_eps, _ptr(text_kv_packed),
                                       _ptr(out), B, rows_per_batch, C, text_len, count, block, scale, _stream()))
     return out
+
+
+def qk_norm_rope(q, k=None, q_gamma=None, k_gamma=None, rot=None, pos=None, eps=1e-6, norm=True, interleaved=True, q_out=None, k_out=None):
+    """Queries [B, T, heads, d] and keys [B, T, kv_heads, d] (or None), normalised per head and rotated by position; returns (q_out, k_out).
+
+    rot [rows, rot_dim / 2, 2] float32: cosine and sine of each position; token t takes row t, or row pos[b, t] (int32; negative:
+    not rotated).  Views of a fused projection are taken as they are, and q_out / k_out may be views (a patch's rows of a stale buffer) or
+    the inputs themselves."""
+    return (_ops or _native()).qk_norm_rope(q, k, q_gamma, k_gamma, rot, pos, eps, int(norm), int(interleaved), q_out, k_out)
+
+
+def kv4_cache(B, L, kv_heads, d, device="cuda"):
+    """An empty 4-bit cache of L rows of keys and values (all zero; see the header for what a row holds)."""
+    n = lib().df_kv4_bytes(B, L, kv_heads, d)
+    if n == 0:
+        raise DfError(f"no 4-bit cache of B={B}, L={L}, kv_heads={kv_heads}, d={d}")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def kv4_refresh(cache, k, v, patch_idx, N):
+    """Rows of patch patch_idx <- k, v [B, L / N, kv_heads, d] (in place); one token of a sequence is patch t of N = L."""
+    return (_ops or _native()).kv4_refresh(cache, k, v, 0, 0, patch_idx, N, SPLIT_ROWS)
+
+
+def kv4_refresh_cols(cache, k, v, H, W, patch_idx, N):
+    """Vertical strip of an H x W token grid: k, v [B, H * W / N, kv_heads, d]."""
+    return (_ops or _native()).kv4_refresh(cache, k, v, H, W, patch_idx, N, SPLIT_COLS)
+
+
+def kv4_read(cache, B, L, kv_heads, d, dtype=torch.bfloat16):
+    """What the rows of a 4-bit cache stand for: k, v [B, L, kv_heads, d] (exact in either type)."""
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise DfError(f"unsupported dtype {dtype}")
+    return (_ops or _native()).kv4_read(cache, B, L, kv_heads, d, DF_BF16 if dtype is torch.bfloat16 else DF_F32)
+
+
+def attn_kv4(q, cache, L, kv_heads, lens=None, scale=None, out=None):
+    """q [B, Lq, heads, d] against a 4-bit cache of L rows (lens [B] int32: the first lens[b] of them; none: zeros) -> [B, Lq, heads, d]."""
+    return (_ops or _native()).attn_kv4(q, cache, L, kv_heads, lens, scale, out)
+
+
+def attn_displaced_kv4(q, k_fresh, v_fresh, cache, patch_idx, N, scale=None, out=None):
+    """attn_displaced with the stale rows in a 4-bit cache: q [B, L / N, heads, d], k_fresh, v_fresh [B, L / N, kv_heads, d]."""
+    return (_ops or _native()).attn_displaced_kv4(q, k_fresh, v_fresh, cache, 0, 0, patch_idx, N, scale, SPLIT_ROWS, out)
+
+
+def attn_displaced_kv4_cols(q, k_fresh, v_fresh, cache, H, W, patch_idx, N, scale=None, out=None):
+    """Vertical strip of an H x W token grid: q, k_fresh, v_fresh hold its H * W / N tokens."""
+    return (_ops or _native()).attn_displaced_kv4(q, k_fresh, v_fresh, cache, H, W, patch_idx, N, scale, SPLIT_COLS, out)
+
+
+def cross_attn(q, k, v, key_mask=None, lens=None, scale=None, out=None):
+    """q [B, Lq, heads, d] against an encoder's k, v [B, Lk, kv_heads, d] (views are taken as they are) -> [B, Lq, heads, d].
+
+    key_mask [B, Lk] bool: False is no key, whatever k and v hold there; lens [B] int32: the first lens[b] are keys.  No key: zeros."""
+    return (_ops or _native()).cross_attn(q, k, v, key_mask, lens, scale, out)
 
 
 def mfma_probe(blocks=2048, iters=4096):

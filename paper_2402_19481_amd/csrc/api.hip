@@ -3,6 +3,7 @@
 #include <mutex>
 
 #include "kernels.h"
+#include "kv4.h"
 
 namespace df {
 
@@ -306,6 +307,151 @@ int df_linear_packed_scratch(const void* xp, const void* wp, const float* bias, 
   a.Xp = xp; a.Wp = wp; a.M = M; a.N = N; a.K = K; a.bias = bias; a.residual = residual; a.ldr = N; a.out_f32 = y_f32;
   a.ldo = N; a.out_packed = y_packed; a.out_rows = y_rows; a.ld_rows = N; a.scr = &s;
   return launch_wgemm(a, (hipStream_t)stream);
+}
+
+int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, void* q_out,
+                    long long qo_ld, long long qo_bs, void* k_out, long long ko_ld, long long ko_bs, const float* q_gamma,
+                    const float* k_gamma, const float* rot, const int* pos, int B, int T, int heads, int kv_heads, int d,
+                    int rot_dim, int rot_len, int norm, float eps, int interleaved, int dtype, void* stream) {
+  if (!q || !q_out || (!k) != (!k_out) || bad_dtype(dtype)) return DF_EINVAL;
+  if (!norm && !rot) return DF_EINVAL;
+  if (norm && !(eps >= 0.f && eps < INFINITY)) return DF_EINVAL;
+  if (B <= 0 || T <= 0 || heads <= 0 || (k ? kv_heads <= 0 : kv_heads != 0)) return DF_ESHAPE;
+  if (d <= 0 || d % 8 || d > 256 || heads > (1 << 20) || kv_heads > (1 << 20)) return DF_ESHAPE;
+  if (rot && (rot_dim <= 0 || rot_dim % 8 || rot_dim > d || rot_len <= 0 || (!pos && rot_len < T))) return DF_ESHAPE;
+  if (q_ld < 0 || q_bs < 0 || k_ld < 0 || k_bs < 0 || qo_ld < 0 || qo_bs < 0 || ko_ld < 0 || ko_bs < 0) return DF_EINVAL;
+  if ((uintptr_t)pos % 4) return DF_EINVAL;
+  // an output's rows must not lie on each other
+  if ((T > 1 && qo_ld < (long long)heads * d) || (B > 1 && qo_bs < (long long)heads * d)) return DF_EINVAL;
+  if (k && ((T > 1 && ko_ld < (long long)kv_heads * d) || (B > 1 && ko_bs < (long long)kv_heads * d))) return DF_EINVAL;
+  RopeArgs a = {};
+  a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out;
+  a.ldq = q_ld; a.bsq = q_bs; a.ldqo = qo_ld; a.bsqo = qo_bs;
+  if (k) { a.ldk = k_ld; a.bsk = k_bs; a.ldko = ko_ld; a.bsko = ko_bs; }
+  a.q_gamma = q_gamma; a.k_gamma = k_gamma; a.rot = rot; a.pos = rot ? pos : nullptr;
+  a.B = B; a.T = T; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.rot_dim = rot_dim; a.rot_len = rot_len;
+  a.norm = norm; a.eps = eps; a.interleaved = interleaved; a.dtype = dtype;
+  return launch_qk_norm_rope(a, (hipStream_t)stream);
+}
+
+// Sizes of a 4-bit cache that the kernels take
+static inline bool kv4_sizes(long long B, long long L, int kv_heads, int d) {
+  return B > 0 && L > 0 && kv_heads > 0 && B <= 65535 && kv_heads <= 65535 && L <= 0x7fffffffLL - 63 && (d == 64 || d == 128);
+}
+
+size_t df_kv4_bytes(int B, int L, int kv_heads, int d) { return kv4_sizes(B, L, kv_heads, d) ? kv4_bytes(B, L, kv_heads, d) : 0; }
+
+// The patch's rows of a grid of H x W tokens (DF_OK, or why not)
+static int own_rows(int H, int W, int patch_idx, int N, int split_axis, int* lo, int* n, int* period) {
+  if (split_axis != DF_SPLIT_ROWS && split_axis != DF_SPLIT_COLS) return DF_EINVAL;
+  if (H <= 0 || W <= 0 || N <= 0 || (long long)H * W > 0x7fffffffLL - 63 || patch_idx < 0 || patch_idx >= N) return DF_ESHAPE;
+  if ((split_axis == DF_SPLIT_ROWS ? ((long long)H * W) % N : W % N)) return DF_ESHAPE;
+  *period = split_axis == DF_SPLIT_ROWS ? 0 : W;
+  *n = split_axis == DF_SPLIT_ROWS ? (int)((long long)H * W / N) : W / N;
+  *lo = patch_idx * *n;
+  return DF_OK;
+}
+// Rows of d values that 16-byte loads take
+static inline bool bad_rows(const void* p, long long ld, long long bs, int dtype) {
+  const int v = dtype == DF_BF16 ? 8 : 4;
+  return (uintptr_t)p % 16 || ld < 0 || bs < 0 || ld % v || bs % v;
+}
+
+int df_kv4_refresh(void* cache, const void* k, long long k_ld, long long k_bs, const void* v, long long v_ld, long long v_bs, int B,
+                   int H, int W, int kv_heads, int d, int patch_idx, int N, int dtype, int split_axis, void* stream) {
+  if (!cache || !k || !v || bad_dtype(dtype) || (uintptr_t)cache % 16 || bad_rows(k, k_ld, k_bs, dtype) || bad_rows(v, v_ld, v_bs, dtype))
+    return DF_EINVAL;
+  Kv4Args a = {};
+  const int rc = own_rows(H, W, patch_idx, N, split_axis, &a.own_lo, &a.own_n, &a.own_period);
+  if (rc != DF_OK) return rc;
+  if (!kv4_sizes(B, (long long)H * W, kv_heads, d)) return DF_ESHAPE;
+  a.cache = cache; a.k = k; a.v = v; a.ldk = k_ld; a.bsk = k_bs; a.ldv = v_ld; a.bsv = v_bs;
+  a.B = B; a.L = H * W; a.kv_heads = kv_heads; a.d = d; a.dtype = dtype;
+  return launch_kv4_refresh(a, (hipStream_t)stream);
+}
+
+int df_kv4_read(const void* cache, void* k, void* v, int B, int L, int kv_heads, int d, int dtype, void* stream) {
+  if (!cache || !k || !v || bad_dtype(dtype) || ((uintptr_t)cache | (uintptr_t)k | (uintptr_t)v) % 16) return DF_EINVAL;
+  if (!kv4_sizes(B, L, kv_heads, d)) return DF_ESHAPE;
+  Kv4Args a = {};
+  a.cache = const_cast<void*>(cache); a.B = B; a.L = L; a.kv_heads = kv_heads; a.d = d; a.dtype = dtype;
+  return launch_kv4_read(a, k, v, (hipStream_t)stream);
+}
+
+// Shapes that the attention kernels take
+static inline int qattn_sizes(int B, int Lq, long long L, int heads, int kv_heads, int d) {
+  if (B <= 0 || B > 65535 || Lq <= 0 || L <= 0 || L > 0x7fffffffLL - 63 || heads <= 0 || kv_heads <= 0 || kv_heads > 65535 || heads % kv_heads)
+    return DF_ESHAPE;
+  if (d <= 0 || d % 8 || d > 128 || heads > (1 << 20) || (long long)Lq * (heads / kv_heads) > 0x7fffffffLL - 256) return DF_ESHAPE;
+  return (long long)B * Lq * heads * (d / 8) < (1LL << 32) - 256 ? DF_OK : DF_ESHAPE;
+}
+static inline bool bad_workspace(const void* w) { return (uintptr_t)w % 256 != 0; }
+
+size_t df_cross_attn_workspace_bytes(int B, int Lq, int Lk, int heads, int kv_heads, int d, int masked, int dtype) {
+  if (bad_dtype(dtype) || qattn_sizes(B, Lq, Lk, heads, kv_heads, d) != DF_OK) return 0;
+  return qattn_workspace(B, (long long)Lq * (heads / kv_heads), kv_heads, d, Lk, 0, false, masked != 0, dtype);
+}
+
+int df_cross_attn(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, const void* v, long long v_ld,
+                  long long v_bs, const unsigned char* key_mask, const int* lens, void* out, int B, int Lq, int Lk, int heads, int kv_heads,
+                  int d, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k || !v || !out || bad_dtype(dtype) || !(scale > 0.f && scale < INFINITY)) return DF_EINVAL;
+  if (bad_rows(q, q_ld, q_bs, dtype) || bad_rows(k, k_ld, k_bs, dtype) || bad_rows(v, v_ld, v_bs, dtype)) return DF_EINVAL;
+  if ((uintptr_t)out % 16 || (uintptr_t)lens % 4 || bad_workspace(workspace)) return DF_EINVAL;
+  const int rc = qattn_sizes(B, Lq, Lk, heads, kv_heads, d);
+  if (rc != DF_OK) return rc;
+  QAttnArgs a = {};
+  a.q = q; a.k = k; a.v = v; a.out = out; a.mask = key_mask; a.lens = lens;
+  a.ldq = q_ld; a.bsq = q_bs; a.ldk = k_ld; a.bsk = k_bs; a.ldv = v_ld; a.bsv = v_bs;
+  a.B = B; a.Lq = Lq; a.L = Lk; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.dtype = dtype; a.scale = scale;
+  a.workspace = workspace; a.workspace_bytes = workspace_bytes;
+  return launch_qattn(a, (hipStream_t)stream);
+}
+
+size_t df_attn_kv4_workspace_bytes(int B, int Lq, int L, int heads, int kv_heads, int d, int dtype) {
+  if (bad_dtype(dtype) || !kv4_sizes(B, L, kv_heads, d) || qattn_sizes(B, Lq, L, heads, kv_heads, d) != DF_OK) return 0;
+  return qattn_workspace(B, (long long)Lq * (heads / kv_heads), kv_heads, d, L, 0, true, false, dtype);
+}
+
+int df_attn_kv4(const void* q, long long q_ld, long long q_bs, const void* cache, const int* lens, void* out, int B, int Lq, int L, int heads,
+                int kv_heads, int d, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !cache || !out || bad_dtype(dtype) || !(scale > 0.f && scale < INFINITY) || bad_rows(q, q_ld, q_bs, dtype)) return DF_EINVAL;
+  if (((uintptr_t)out | (uintptr_t)cache) % 16 || (uintptr_t)lens % 4 || bad_workspace(workspace)) return DF_EINVAL;
+  if (!kv4_sizes(B, L, kv_heads, d)) return DF_ESHAPE;
+  const int rc = qattn_sizes(B, Lq, L, heads, kv_heads, d);
+  if (rc != DF_OK) return rc;
+  QAttnArgs a = {};
+  a.q = q; a.cache = cache; a.out = out; a.lens = lens; a.ldq = q_ld; a.bsq = q_bs;
+  a.B = B; a.Lq = Lq; a.L = L; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.dtype = dtype; a.scale = scale;
+  a.workspace = workspace; a.workspace_bytes = workspace_bytes;
+  return launch_qattn(a, (hipStream_t)stream);
+}
+
+size_t df_attn_displaced_kv4_workspace_bytes(int B, int H, int W, int heads, int kv_heads, int d, int N, int dtype) {
+  if (H <= 0 || W <= 0 || N <= 0 || ((long long)H * W) % N || bad_dtype(dtype) || !kv4_sizes(B, (long long)H * W, kv_heads, d)) return 0;
+  const int L = H * W, own = L / N;
+  if (qattn_sizes(B, own, L, heads, kv_heads, d) != DF_OK) return 0;
+  return qattn_workspace(B, (long long)own * (heads / kv_heads), kv_heads, d, L - own, own, true, false, dtype);
+}
+
+int df_attn_displaced_kv4(const void* q, long long q_ld, long long q_bs, const void* k_fresh, long long k_ld, long long k_bs, const void* v_fresh,
+                          long long v_ld, long long v_bs, const void* cache, void* out, int B, int H, int W, int heads, int kv_heads, int d,
+                          int patch_idx, int N, float scale, int dtype, int split_axis, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k_fresh || !v_fresh || !cache || !out || bad_dtype(dtype) || !(scale > 0.f && scale < INFINITY)) return DF_EINVAL;
+  if (bad_rows(q, q_ld, q_bs, dtype) || bad_rows(k_fresh, k_ld, k_bs, dtype) || bad_rows(v_fresh, v_ld, v_bs, dtype)) return DF_EINVAL;
+  if (((uintptr_t)out | (uintptr_t)cache) % 16 || bad_workspace(workspace)) return DF_EINVAL;
+  QAttnArgs a = {};
+  int rc = own_rows(H, W, patch_idx, N, split_axis, &a.own_lo, &a.own_n, &a.own_period);
+  if (rc != DF_OK) return rc;
+  if (!kv4_sizes(B, (long long)H * W, kv_heads, d)) return DF_ESHAPE;
+  a.L = H * W; a.Lq = a.L / N;
+  rc = qattn_sizes(B, a.Lq, a.L, heads, kv_heads, d);
+  if (rc != DF_OK) return rc;
+  a.q = q; a.k = k_fresh; a.v = v_fresh; a.cache = cache; a.out = out;
+  a.ldq = q_ld; a.bsq = q_bs; a.ldk = k_ld; a.bsk = k_bs; a.ldv = v_ld; a.bsv = v_bs;
+  a.B = B; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.dtype = dtype; a.scale = scale;
+  a.workspace = workspace; a.workspace_bytes = workspace_bytes;
+  return launch_qattn(a, (hipStream_t)stream);
 }
 
 int df_euler_update(float* x, const float* eps, float sigma, float sigma_next, long long n, void* stream) {

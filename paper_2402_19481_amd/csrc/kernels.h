@@ -248,4 +248,50 @@ size_t sync_probe_bytes(int blocks);
 int launch_sync_probe(void* buf, int blocks, int iters, int mode, hipStream_t st);
 int launch_scale(float* y, const float* x, float alpha, long long n, hipStream_t st);
 
+// ---- qkrope.hip ----
+// Strides are elements between tokens (ld) and batch items (bs); a token's heads lie side by side.
+struct RopeArgs {
+  const void *q, *k;      // [B, T, heads, d], [B, T, kv_heads, d]; k may be null (kv_heads 0)
+  void *q_out, *k_out;    // may be the inputs themselves
+  long long ldq, bsq, ldk, bsk, ldqo, bsqo, ldko, bsko;
+  const float *q_gamma, *k_gamma;   // [d] or null: no scale
+  const float* rot;       // [rot_len][rot_dim / 2][2] cosine and sine, or null: no rotation
+  const int* pos;         // [B, T] or null: token t turns by row t
+  int B, T, heads, kv_heads, d, rot_dim, rot_len, norm, interleaved, dtype;
+  float eps;
+};
+int launch_qk_norm_rope(const RopeArgs& a, hipStream_t st);
+
+// ---- kv4.hip ----
+struct Kv4Args {
+  void* cache;            // kv4.h
+  const void *k, *v;      // fresh rows, strides as above
+  long long ldk, bsk, ldv, bsv;
+  int B, L, kv_heads, d, dtype;
+  int own_lo, own_n, own_period;   // as AttnArgs
+};
+int launch_kv4_refresh(const Kv4Args& a, hipStream_t st);
+int launch_kv4_read(const Kv4Args& a, void* k, void* v, hipStream_t st);
+// Rows that are not the patch's, in their order, `rows` per head, as bf16 [B][kv_heads][rows][d]; lens [B] or null: rows from there on may stay
+int launch_kv4_expand(const Kv4Args& a, const int* lens, long long rows, void* k, void* v, hipStream_t st);
+
+// ---- qattn.hip ----
+struct QAttnArgs {
+  const void* q;          // [B, Lq, heads, d], strides as above
+  const void *k, *v;      // [B, L, kv_heads, d]; beside a cache: the patch's own rows, or null with own_n == 0
+  const void* cache;      // L rows (kv4.h), or null
+  void* out;              // [B, Lq, heads, d]
+  const unsigned char* mask;   // [B, L] or null (no cache)
+  const int* lens;        // [B] or null (own_n == 0)
+  long long ldq, bsq, ldk, bsk, ldv, bsv;
+  int B, Lq, L, heads, kv_heads, d, dtype;
+  int own_lo, own_n, own_period;
+  float scale;
+  void* workspace;        // qattn_workspace bytes, 256-byte aligned
+  size_t workspace_bytes;
+};
+// rows: Lq * (heads / kv_heads); keys0: rows of the cache that are not the patch's, or all keys; keys1: the patch's own rows beside a cache
+size_t qattn_workspace(int B, long long rows, int kv_heads, int d, long long keys0, long long keys1, bool cached, bool masked, int dtype);
+int launch_qattn(const QAttnArgs& a, hipStream_t st);
+
 }  // namespace df

@@ -1,0 +1,80 @@
+"""Attention to an encoder's states of another length against the 64-bit form (bounds derived there)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_19481_amd as df
+from oracle import block_ops as bo
+from gpu_util import DEV, host
+
+pytestmark = pytest.mark.gpu
+TYPES = {True: torch.bfloat16, False: torch.float32}
+
+
+def _rows(seed, *shape, bf16=True, std=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std).to(TYPES[bf16]).to(DEV)
+
+
+def _check(got, q, k, v, bf16, valid=None, scale=None):
+    d = q.shape[-1]
+    if valid is not None:                                    # what lies in masked places must not matter to the reference either
+        k, v = np.where(valid[:, :, None, None], k, 0), np.where(valid[:, :, None, None], v, 0)
+    ref, size, reach = bo.attention(host(q), k, v, d ** -0.5 if scale is None else scale, valid)
+    off = np.abs(host(got) - ref)
+    bound = bo.attention_bound(ref, size, reach, d, k.shape[1], bf16)
+    assert (off <= bound).all(), (np.argwhere(~(off <= bound))[:4], off.max(), float((off / bound).max()))
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("B,Lq,Lk,heads,kv,d", [
+    (1, 1, 1, 1, 1, 64), (1, 1, 77, 20, 20, 64), (2, 300, 77, 4, 4, 64), (1, 129, 64, 2, 2, 64), (2, 31, 300, 4, 2, 128), (1, 257, 130, 2, 2, 128),
+    (1, 40, 65, 3, 3, 72), (1, 50, 200, 2, 1, 40), (1, 20, 33, 2, 2, 32), (1, 33, 500, 1, 1, 96), (1, 2, 3000, 2, 1, 64), (1, 9, 128, 1, 1, 8),
+])
+def test_lengths_and_masks(B, Lq, Lk, heads, kv, d, bf16):
+    print("cross", B, Lq, Lk, heads, kv, d, bf16, flush=True)
+    q = _rows(1, B, Lq, heads, d, bf16=bf16, std=1.5)
+    fused = _rows(2, B, Lk, 2 * kv * d, bf16=bf16)
+    k, v = fused[..., :kv * d].unflatten(-1, (kv, d)), fused[..., kv * d:].unflatten(-1, (kv, d))
+    _check(df.cross_attn(q, k, v), q, host(k), host(v), bf16)
+    _check(df.cross_attn(q, k, v, scale=2.5), q, host(k), host(v), bf16, scale=2.5)
+    mask = torch.rand(B, Lk, generator=torch.Generator().manual_seed(9)) < 0.6
+    mask[0, :70] = False                                     # a tile without a key in front (short prompts: none at all)
+    lens = torch.tensor([Lk, max(1, Lk // 3)][:B], dtype=torch.int32)
+    within = torch.arange(Lk)[None] < lens[:, None]
+    for m, n in ((mask, None), (None, lens), (mask, lens)):
+        valid = (m if m is not None else torch.ones(B, Lk, dtype=torch.bool)) & (within if n is not None else True)
+        f = fused.clone()
+        f[~valid.to(DEV)] = float("nan")
+        k, v = f[..., :kv * d].unflatten(-1, (kv, d)), f[..., kv * d:].unflatten(-1, (kv, d))
+        got = df.cross_attn(q, k, v, key_mask=None if m is None else m.to(DEV), lens=None if n is None else n.to(DEV))
+        _check(got, q, host(k), host(v), bf16, valid.numpy())
+        if not valid[0].any():
+            assert not got[0].any()
+    if m is not None:
+        assert torch.equal(got, df.cross_attn(q, k, v, key_mask=m.to(torch.uint8).to(DEV) * 255, lens=lens.to(DEV)))
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_scores_far_apart_and_without_a_number(bf16):
+    B, Lq, Lk, d = 1, 40, 400, 64
+    q, k, v = _rows(1, B, Lq, 1, d, bf16=bf16, std=8.0), _rows(2, B, Lk, 1, d, bf16=bf16, std=8.0), _rows(3, B, Lk, 1, d, bf16=bf16)
+    k = k * torch.linspace(0.1, 3, Lk, device=DEV)[None, :, None, None].to(k.dtype)    # the maximum climbs tile by tile
+    got, kh = df.cross_attn(q, k, v), host(k)
+    ref, size, reach = bo.attention(host(q), kh, host(v), d ** -0.5)
+    assert reach > 300                                       # (the bound has the score's own error, which is not small here)
+    assert (np.abs(host(got) - ref) <= bo.attention_bound(ref, size, reach, d, Lk, bf16)).all()
+    lens = torch.tensor([7], dtype=torch.int32, device=DEV)
+    w = k.clone()
+    w[0, 3, 0, 0], w[0, 9] = float("nan"), float("nan")
+    assert df.cross_attn(q, w, v, lens=lens).isnan().all()   # a key without a number counts, one behind the length does not
+    w[0, 3] = k[0, 3]
+    _check(df.cross_attn(q, w, v, lens=lens), q, kh, host(v), bf16, np.arange(Lk)[None] < 7)
+    w[0, :7] = float("-inf")
+    assert df.cross_attn(q.abs(), w, v, lens=lens).isnan().all()                       # every score -inf: the formula has no value
+
+
+def test_the_same_bits_and_a_given_result():
+    q, k, v = _rows(1, 2, 50, 4, 64), _rows(2, 2, 900, 2, 64), _rows(3, 2, 900, 2, 64)
+    out = torch.empty_like(q)
+    assert df.cross_attn(q, k, v, out=out) is out
+    assert all(torch.equal(out, df.cross_attn(q, k, v)) for _ in range(3))
