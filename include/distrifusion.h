@@ -301,7 +301,7 @@ int df_kv4_read(const void* cache, void* k, void* v, int B, int L, int kv_heads,
 size_t df_attn_kv4_workspace_bytes(int B, int Lq, int L, int heads, int kv_heads, int d, int dtype);
 int df_attn_kv4(const void* q, long long q_ld, long long q_bs, const void* cache, const int* lens, void* out, int B, int Lq, int L, int heads,
                 int kv_heads, int d, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream);
-size_t df_attn_displaced_kv4_workspace_bytes(int B, int H, int W, int heads, int kv_heads, int d, int N, int dtype);
+size_t df_attn_displaced_kv4_workspace_bytes(int B, int H, int W, int heads, int kv_heads, int d, int patch_idx, int N, int dtype, int split_axis);
 int df_attn_displaced_kv4(const void* q, long long q_ld, long long q_bs, const void* k_fresh, long long k_ld, long long k_bs, const void* v_fresh,
                           long long v_ld, long long v_bs, const void* cache, void* out, int B, int H, int W, int heads, int kv_heads, int d,
                           int patch_idx, int N, float scale, int dtype, int split_axis, void* workspace, size_t workspace_bytes, void* stream);

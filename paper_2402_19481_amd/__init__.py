@@ -83,7 +83,7 @@ def lib():
     L.df_attn_kv4.argtypes = [vp, ll, ll, vp, vp, vp, i, i, i, i, i, i, f, i, vp, sz, vp]
     L.df_attn_kv4_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
     L.df_attn_displaced_kv4.argtypes = [vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, i, i, i, i, i, i, i, i, f, i, i, vp, sz, vp]
-    L.df_attn_displaced_kv4_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+    L.df_attn_displaced_kv4_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i, i, i]
     L.df_cross_attn.argtypes = [vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, vp, i, i, i, i, i, i, f, i, vp, sz, vp]
     L.df_cross_attn_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
     for name in ("df_kv4_bytes", "df_attn_kv4_workspace_bytes", "df_attn_displaced_kv4_workspace_bytes", "df_cross_attn_workspace_bytes"):

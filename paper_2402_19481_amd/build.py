@@ -14,6 +14,10 @@ SOURCES = ["api.hip", "refresh.hip", "groupnorm.hip", "conv_gemm.hip", "tgemm.hi
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-mllvm", "-amdgpu-kernarg-preload-count=16"]
 
+# The attention of qattn.hip keeps one wave of up to 512 registers per SIMD.  Left alone the compiler then puts every matrix accumulator in the
+# half of them that vector instructions cannot read, and copies the scores out, as many instructions as the exponentials.
+SOURCE_FLAGS = {"qattn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 # The tuning build (python -m paper_2402_19481_amd.build --tuning) compiles the environment switches in (DF_TG,
 # DF_TGS, DF_ATTN_SPLITS, ...: kernel-selection overrides for sweeps such as `bench.py --tile-sweep`) and writes
@@ -44,7 +48,7 @@ def _compile_binding():
 
 def _compile(src, tuning=False):
     obj = os.path.join(OBJ_TUNE if tuning else OBJ, src.replace(".hip", ".o"))
-    cmd = ["hipcc", *FLAGS, *(["-DDF_TUNING"] if tuning else []), "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = ["hipcc", *FLAGS, *SOURCE_FLAGS.get(src, []), *(["-DDF_TUNING"] if tuning else []), "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:

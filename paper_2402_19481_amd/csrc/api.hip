@@ -389,7 +389,7 @@ static inline bool bad_workspace(const void* w) { return (uintptr_t)w % 256 != 0
 
 size_t df_cross_attn_workspace_bytes(int B, int Lq, int Lk, int heads, int kv_heads, int d, int masked, int dtype) {
   if (bad_dtype(dtype) || qattn_sizes(B, Lq, Lk, heads, kv_heads, d) != DF_OK) return 0;
-  return qattn_workspace(B, (long long)Lq * (heads / kv_heads), kv_heads, d, Lk, 0, false, masked != 0, dtype);
+  return qattn_workspace(B, (long long)Lq * (heads / kv_heads), kv_heads, d, Lk, 0, 0, false, false, masked != 0, dtype);
 }
 
 int df_cross_attn(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, const void* v, long long v_ld,
@@ -410,7 +410,7 @@ int df_cross_attn(const void* q, long long q_ld, long long q_bs, const void* k, 
 
 size_t df_attn_kv4_workspace_bytes(int B, int Lq, int L, int heads, int kv_heads, int d, int dtype) {
   if (bad_dtype(dtype) || !kv4_sizes(B, L, kv_heads, d) || qattn_sizes(B, Lq, L, heads, kv_heads, d) != DF_OK) return 0;
-  return qattn_workspace(B, (long long)Lq * (heads / kv_heads), kv_heads, d, L, 0, true, false, dtype);
+  return qattn_workspace(B, (long long)Lq * (heads / kv_heads), kv_heads, d, L, 0, 0, false, true, false, dtype);
 }
 
 int df_attn_kv4(const void* q, long long q_ld, long long q_bs, const void* cache, const int* lens, void* out, int B, int Lq, int L, int heads,
@@ -427,11 +427,12 @@ int df_attn_kv4(const void* q, long long q_ld, long long q_bs, const void* cache
   return launch_qattn(a, (hipStream_t)stream);
 }
 
-size_t df_attn_displaced_kv4_workspace_bytes(int B, int H, int W, int heads, int kv_heads, int d, int N, int dtype) {
-  if (H <= 0 || W <= 0 || N <= 0 || ((long long)H * W) % N || bad_dtype(dtype) || !kv4_sizes(B, (long long)H * W, kv_heads, d)) return 0;
+size_t df_attn_displaced_kv4_workspace_bytes(int B, int H, int W, int heads, int kv_heads, int d, int patch_idx, int N, int dtype, int split_axis) {
+  int lo, n, period;
+  if (bad_dtype(dtype) || own_rows(H, W, patch_idx, N, split_axis, &lo, &n, &period) != DF_OK || !kv4_sizes(B, (long long)H * W, kv_heads, d)) return 0;
   const int L = H * W, own = L / N;
   if (qattn_sizes(B, own, L, heads, kv_heads, d) != DF_OK) return 0;
-  return qattn_workspace(B, (long long)own * (heads / kv_heads), kv_heads, d, L - own, own, true, false, dtype);
+  return qattn_workspace(B, (long long)own * (heads / kv_heads), kv_heads, d, L, own, lo, period > 0, true, false, dtype);
 }
 
 int df_attn_displaced_kv4(const void* q, long long q_ld, long long q_bs, const void* k_fresh, long long k_ld, long long k_bs, const void* v_fresh,

@@ -127,7 +127,7 @@ using AttnKv4Fn = int (*)(const void*, long long, long long, const void*, const 
 using AttnKv4BytesFn = size_t (*)(int, int, int, int, int, int, int);
 using DisplacedKv4Fn = int (*)(const void*, long long, long long, const void*, long long, long long, const void*, long long, long long, const void*,
                                void*, int, int, int, int, int, int, int, int, float, int, int, void*, size_t, void*);
-using DisplacedKv4BytesFn = size_t (*)(int, int, int, int, int, int, int, int);
+using DisplacedKv4BytesFn = size_t (*)(int, int, int, int, int, int, int, int, int, int);
 using CrossFn = int (*)(const void*, long long, long long, const void*, long long, long long, const void*, long long, long long,
                         const unsigned char*, const int*, void*, int, int, int, int, int, int, float, int, void*, size_t, void*);
 using CrossBytesFn = size_t (*)(int, int, int, int, int, int, int, int);
@@ -545,7 +545,7 @@ PyObject* attn_displaced_kv4(PyObject*, PyObject* const* a, Py_ssize_t na) {
     int rc;
     {
       Released r;
-      const size_t bytes = g_displaced_kv4_bytes(h.B, H, W, h.H, hk.H, h.d, N, h.dt);
+      const size_t bytes = g_displaced_kv4_bytes(h.B, H, W, h.H, hk.H, h.d, patch, N, h.dt, axis);
       const at::Tensor w = workspace(q, bytes);
       rc = g_displaced_kv4(h.p, h.ld, h.bs, hk.p, hk.ld, hk.bs, hv.p, hv.ld, hv.bs, c, out.data_ptr(), h.B, H, W, h.H, hk.H, h.d, patch, N, scale, h.dt,
                            axis, address(w), bytes, stream());

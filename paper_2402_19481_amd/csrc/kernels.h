@@ -290,8 +290,9 @@ struct QAttnArgs {
   void* workspace;        // qattn_workspace bytes, 256-byte aligned
   size_t workspace_bytes;
 };
-// rows: Lq * (heads / kv_heads); keys0: rows of the cache that are not the patch's, or all keys; keys1: the patch's own rows beside a cache
-size_t qattn_workspace(int B, long long rows, int kv_heads, int d, long long keys0, long long keys1, bool cached, bool masked, int dtype);
+// rows: Lq * (heads / kv_heads); own: how many of the L keys are the patch's own rows beside a cache, from own_lo on (period: not in a row)
+size_t qattn_workspace(int B, long long rows, int kv_heads, int d, long long L, long long own, long long own_lo, bool period, bool cached, bool masked,
+                       int dtype);
 int launch_qattn(const QAttnArgs& a, hipStream_t st);
 
 }  // namespace df

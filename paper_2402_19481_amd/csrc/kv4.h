@@ -54,4 +54,11 @@ __device__ __forceinline__ unsigned int kv4_codes(unsigned int old, float x0, fl
 template <int SEL>
 __device__ __forceinline__ f32x2 kv4_levels(unsigned int w) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, SEL); }
 
+// What eight codes stand for
+__device__ __forceinline__ void kv4_values(unsigned int w, float s, float* o) {
+  const f32x2 a[4] = {kv4_levels<0>(w), kv4_levels<1>(w), kv4_levels<2>(w), kv4_levels<3>(w)};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = a[i >> 1][i & 1] * s;
+}
+
 }  // namespace df

@@ -120,13 +120,6 @@ __global__ __launch_bounds__(256) void kv4_refresh_kernel(Kv4Params p) {
   }
 }
 
-// What eight codes stand for
-__device__ __forceinline__ void values8(unsigned int w, float s, float* o) {
-  const f32x2 a[4] = {kv4_levels<0>(w), kv4_levels<1>(w), kv4_levels<2>(w), kv4_levels<3>(w)};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) o[i] = a[i >> 1][i & 1] * s;
-}
-
 // A tile of V codes -> dwords of eight values of a key, at [key][D / 8 + 1]: 8 x 8 nibbles turn per eight values and eight keys
 template <int D>
 __device__ __forceinline__ void turn_values(const unsigned char* vt, unsigned int* vw, int tid) {
@@ -172,7 +165,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Params p) {
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       float o[8];
-      values8(kv ? vw[r * PITCH + sub] : kw[i], s[i][kv], o);
+      kv4_values(kv ? vw[r * PITCH + sub] : kw[i], s[i][kv], o);
       st8((T*)(kv ? p.vo : p.ko) + to, o);
     }
   }
@@ -214,7 +207,7 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(Kv4Params p, const int*
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       float o[8];
-      values8(kv ? vw[r * PITCH + sub] : kw[i], s[i][kv], o);
+      kv4_values(kv ? vw[r * PITCH + sub] : kw[i], s[i][kv], o);
       st_vec((bf16_t*)(kv ? p.vo : p.ko) + to, o);
     }
   }

@@ -9,6 +9,8 @@
 // by the order in which keys are assigned to its rows, the operand P^T without any data movement).  P is rounded to bf16 as the matrix
 // instruction takes it (2^-9 of each weight, averaged over the keys); sums, maxima and O are float, the row sums are those of the float weights.
 // float: the same on v_mfma_f32_32x32x2_f32, for the small full-precision networks.
+#include <cstring>
+
 #include "kv4.h"
 
 namespace df {
@@ -16,6 +18,8 @@ namespace df {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLow = -3.0e38f;               // a running maximum before the first score: finite, so that -inf scores have weight 0
+#define DF_INLINE __attribute__((always_inline))
 
 struct Seg {
   const void *k, *v;                           // rows of d values
@@ -69,127 +73,749 @@ __device__ __forceinline__ void place(const QParams& p, int nrb, int& rb, int& k
 constexpr int kListTiles = 1024;               // tiles of one split whose words are kept (masks)
 
 // ---- bf16 rows ----
-template <int D, int NW, bool MASK>
-__global__ __launch_bounds__(64 * NW, 2) void rows_attn(QParams p) {
-  constexpr int TK = 64, TILE = TK * D * 2, CH = D / 8, KS = D / 16, DB = D / 32, LPT = TILE / 1024 / NW, RPI = 1024 / (D * 2);
-  static_assert(LPT >= 1, "a wave loads a part of each tile");
-  extern __shared__ __attribute__((aligned(16))) char smem[];             // three slots of a K and a V tile; MASK: words and tiles
+// A workgroup is four waves of QB * 32 rows.  The work is a line of tiles of 64 keys, block of rows by block of rows; workgroup w takes the w-th of
+// equal shares of it (`Share`), so all end together whatever the number of blocks: a share that covers a block writes its result, one that
+// begins or ends inside a block leaves a part (running maximum, sum, O in float) for merge_shares.
+struct Share {
+  unsigned int tiles, count, per, more, all;   // tiles of a block; shares; each `per` tiles, the first `more` one more, the last what is left of all
+};
+__host__ __device__ inline unsigned int share_begin(const Share& s, unsigned int w) {
+  const unsigned int t = w * s.per + (w < s.more ? w : s.more);
+  return t < s.all ? t : s.all;
+}
+__host__ __device__ inline unsigned int share_of(const Share& s, unsigned int tile) {
+  const unsigned int big = s.more * (s.per + 1);
+  return tile < big ? tile / (s.per + 1) : s.more + (tile - big) / s.per;
+}
+
+// The loop is software-pipelined inside the wave, since matrix instructions and the softmax's vector instructions of a SIMD overlap only where one
+// wave's stream mixes them: iteration t issues S_{t+1} = K_{t+1} Q^T and O += V_{t-1} P_{t-1} between the exponentials of tile t, whose registers
+// take S_{t+1} as they come free.  K and V tiles go memory -> LDS by direct loads, K_{t+3} and V_{t+1} in iteration t, to rings of four slots (so
+// that K_t is there to the end of iteration t, and all slots follow from one number).  With one wave on a SIMD every instruction takes its time
+// slot, scalar ones too: runs of whole tiles of one segment go through a loop that only moves its pointers on.
+// The running maximum is that of the first tile and moves when a row's weights of a tile sum to more than 2^13 (the sums are needed anyway; the
+// maximum of every tile would be 22 instructions more): by the power of two above the sum, which scales the packed weights exactly, or, beyond 2^100,
+// to the tile's own maximum, with the tile done again from its K in LDS.
+template <int D, int QB, bool MASK>
+__global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QParams p, Share sh) {
+  constexpr int TILE = 64 * D * 2, CH = D / 8, KS = D / 16, DB = D / 32, LPT = TILE / 4096, RPI = 1024 / (D * 2), M = D / 64, BLK = 128 * QB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];             // four K tiles, four V tiles; MASK: words and tiles
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 5, c = lane & 31, csig = (c & 0x13) | ((c & 4) << 1) | ((c & 8) >> 1);
-  int rb, kh, b, split;
-  place(p, (p.rows + 32 * NW - 1) / (32 * NW), rb, kh, b, split);
-  const int n0 = seg0_rows(p, b), n1 = p.seg[1].n, tiles0 = (n0 + 63) >> 6;
-  const int lo = split * p.tiles_per_split;
-  int hi = lo + p.tiles_per_split;
-  if (hi > tiles0 + ((n1 + 63) >> 6)) hi = tiles0 + ((n1 + 63) >> 6);
-  int nt = hi > lo ? hi - lo : 0;
-
-  unsigned long long* words = (unsigned long long*)(smem + 6 * TILE);     // MASK: of the tiles that have a key
-  unsigned short* list = (unsigned short*)(words + kListTiles);
-  if constexpr (MASK) {
-    for (int i = wave; i < nt; i += NW) {
-      const int key = (lo + i) * 64 + lane;
-      const unsigned long long w = __builtin_amdgcn_ballot_w64(key < n0 && p.mask[(long long)b * p.seg[0].n + key] != 0);
-      if (lane == 0) words[i] = w;
-    }
-    __syncthreads();
-    // the tiles with a key move to the front (wave 0; every chunk is read before it is written, in front of itself)
-    if (wave == 0) {
-      int at = 0;
-      for (int i = 0; i < nt; i += 64) {
-        const unsigned long long w = i + lane < nt ? words[i + lane] : 0ULL;
-        const unsigned long long some = __builtin_amdgcn_ballot_w64(w != 0);
-        const int to = at + __popcll(some & low_bits(lane));
-        if (w) { words[to] = w; list[to] = (unsigned short)(i + lane); }
-        at += __popcll(some);
-      }
-      if (lane == 0) *(int*)(list + kListTiles) = at;
-    }
-    __syncthreads();
-    nt = *(volatile int*)(list + kListTiles);
-  }
-  nt = __builtin_amdgcn_readfirstlane(nt);
-
-  const int row = rb * 32 * NW + wave * 32 + c;
-  const bool have = row < p.rows;
-  const bool idle = __builtin_amdgcn_readfirstlane(rb * 32 * NW + wave * 32) >= p.rows;
-  bf16x8 qreg[KS];
+  const int g = lane >> 5, c = lane & 31, csig = (c & 0x13) | ((c & 4) << 1) | ((c & 8) >> 1), tri = lane & 15;
+  const int nrb = (p.rows + BLK - 1) / BLK;
+  unsigned int w;
   {
-    const bf16_t* qp = (const bf16_t*)p.q + row_offset(p, b, kh, have ? row : 0, p.bsq, p.ldq);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      u32x4 t = {0u, 0u, 0u, 0u};
-      if (have && 16 * s + 8 * g < p.d) t = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * g);
-      qreg[s] = __builtin_bit_cast(bf16x8, t);
-    }
+    const unsigned int t = blockIdx.x, xcd = t & 7, base = sh.count >> 3, rem = sh.count & 7;   // an XCD takes shares side by side: the same keys
+    w = xcd * base + (xcd < rem ? xcd : rem) + (t >> 3);
   }
-
-  auto tile_of = [&](int i) { return MASK ? (int)list[i] : i; };
-  auto word_of = [&](int i, int t) {
-    if constexpr (MASK) return words[i];
-    else return t < tiles0 ? low_bits(n0 - t * 64) : low_bits(n1 - (t - tiles0) * 64);
-  };
-  // Direct loads of tile i to slot: keys that are none are read as one that is (their weight is 0, the value must be finite where the others
-  // are); values beyond d are read as the first ones (Q is 0 there, those of O are dropped)
-  auto load = [&](int i, int slot) {
-    const int t = lo + tile_of(i);
-    const unsigned long long w = word_of(i, t);
-    const bool second = !MASK && t >= tiles0;
-    const Seg& s = p.seg[second ? 1 : 0];
-    const int key0 = (second ? t - tiles0 : t) * 64, some = __builtin_ctzll(w);
-    const bf16_t* k = (const bf16_t*)s.k + (long long)b * s.bsk + (long long)kh * s.hsk + (long long)key0 * s.ldk;
-    const bf16_t* v = (const bf16_t*)s.v + (long long)b * s.bsv + (long long)kh * s.hsv + (long long)key0 * s.ldv;
+  unsigned int pos = share_begin(sh, w);
+  const unsigned int end = share_begin(sh, w + 1);
+  unsigned long long* words = (unsigned long long*)(smem + 8 * TILE);     // MASK: of the tiles that have a key
+  unsigned short* list = (unsigned short*)(words + kListTiles);
+  // Direct load j of the wave covers tile rows (LPT wave + j) * RPI + lane / CH; the chunks of a row are swizzled by it.  Values beyond d are read as
+  // the first ones (Q is 0 there, those of O are dropped).
+  unsigned int kch[LPT], vch[LPT];
+  int trow[LPT];
 #pragma unroll
-    for (int j = 0; j < LPT; ++j) {
-      const int r = (wave * LPT + j) * RPI + lane / CH, at = lane % CH;
-      const int from = (w >> r) & 1 ? r : some;
-      const int kc = (at ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 8;
-      const int vc = (at ^ (D == 64 ? ((r >> 1) & 1) * 2 ^ ((r >> 3) & 1) * 4 : (r & 3) * 4)) * 8;
-      char* to = smem + slot * 2 * TILE + (wave * LPT + j) * 1024;
-      lds_load16(k + (long long)from * s.ldk + (kc < p.d ? kc : 0), to);
-      lds_load16(v + (long long)from * s.ldv + (vc < p.d ? vc : 0), to + TILE);
+  for (int j = 0; j < LPT; ++j) {
+    const int r = (wave * LPT + j) * RPI + lane / CH, at = lane % CH;
+    const int kc = (at ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 8;
+    const int vc = (at ^ (D == 64 ? ((r >> 1) & 1) * 2 ^ ((r >> 3) & 1) * 4 : (r & 3) * 4)) * 8;
+    trow[j] = r;
+    kch[j] = kc < p.d ? 2 * kc : 0;
+    vch[j] = vc < p.d ? 2 * vc : 0;
+  }
+  auto slot_of = [&](int i) DF_INLINE { return (i & 3) * TILE; };
+  constexpr int VR = 4 * TILE;                             // the ring of V
+  const int wofs = 1024 * LPT * wave;
+  // LDS offsets of this lane's operands in a tile: chunk 2 s + g of MFMA row c, which is key csig (the second block of keys is 32 rows on); four keys
+  // of 16 values for the transposing reads (the lane's chunks 1 and 2 exchanged, so that O's rows come out in the order of csig too)
+  const int kof = csig * (D * 2) + ((g ^ (D == 64 ? (csig >> 1) & 7 : csig & 15)) * 16);
+  int vof[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    const int key = 8 * g + (tri >> 2), chunk = 4 * db + 2 * ((lane >> 4) & 1) + (tri & 1);
+    const int pc = D == 64 ? chunk ^ (2 * ((key >> 1) & 1)) ^ (4 * ((key >> 3) & 1)) : chunk ^ ((key & 3) * 4);
+    vof[db] = key * (D * 2) + pc * 16 + ((tri >> 1) & 1) * 8;
+  }
+  auto kfrag = [&](int at, int s, int kb) DF_INLINE { return *reinterpret_cast<const u32x4*>(smem + (at + (kof ^ (32 * s))) + kb * 32 * D * 2); };
+  auto vfrag = [&](int slot, int ts, int db) DF_INLINE {
+    typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+    const char* at = smem + (slot + vof[db]) + VR + ts * 16 * D * 2;
+    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at));
+    const bf16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at + 4 * D * 2));
+    const u32x2 a2 = __builtin_bit_cast(u32x2, a), z2 = __builtin_bit_cast(u32x2, z);
+    return u32x4{a2.x, a2.y, z2.x, z2.y};
+  };
+  auto sync_tile = [&]() DF_INLINE {                                   // all but the last iteration's loads have landed, and its reads are done, for every wave
+    __builtin_amdgcn_s_waitcnt((2 * LPT) | (0x7 << 4) | (0 << 8));
+    block_sync();
+  };
+
+  // A block of rows (or the share's part of one)
+  struct Block { int kh, b, row0, lo, nt, n0, tiles0; bool whole; };
+  auto open = [&]() DF_INLINE {
+    Block r;
+    const unsigned int block = pos / sh.tiles;
+    r.lo = (int)(pos - block * sh.tiles);
+    int hi = (int)(r.lo + end - pos < sh.tiles ? r.lo + end - pos : sh.tiles);
+    pos += hi - r.lo;
+    r.whole = r.lo == 0 && hi == (int)sh.tiles;
+    const int bh = (int)(block / (unsigned int)nrb);
+    r.row0 = ((int)(block % (unsigned int)nrb)) * BLK + wave * 32 * QB;
+    r.b = bh / p.kv_heads;
+    r.kh = bh - r.b * p.kv_heads;
+    r.n0 = seg0_rows(p, r.b);
+    r.tiles0 = (r.n0 + 63) >> 6;
+    if (hi > r.tiles0 + ((p.seg[1].n + 63) >> 6)) hi = r.tiles0 + ((p.seg[1].n + 63) >> 6);
+    r.nt = hi > r.lo ? hi - r.lo : 0;
+    return r;
+  };
+  bf16x8 qreg[QB][KS], qnext[QB][KS];
+  auto queries = [&](const Block& k) DF_INLINE {           // the wave's rows of Q -> qnext
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+      const bool have = k.row0 + 32 * n + c < p.rows;
+      const bf16_t* qp = (const bf16_t*)p.q + row_offset(p, k.b, k.kh, have ? k.row0 + 32 * n + c : 0, p.bsq, p.ldq);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        u32x4 t = {0u, 0u, 0u, 0u};
+        if (have && 16 * s + 8 * g < p.d) t = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * g);
+        qnext[n][s] = __builtin_bit_cast(bf16x8, t);
+      }
     }
   };
 
-  f32x16 o[DB];
+  Block blk = open(), after = blk;
+  bool primed = false;                                     // the last block's final iterations have requested this one's first tiles and Q
+  int s0 = 0;                                              // slot of its tile 0
+  int listed = 0;                                          // MASK: tiles of the list
+  for (bool more = true, same = false; more;) {
+    more = pos < end;
+    if (more) after = open();
+    if (!primed) queries(blk);
+    if constexpr (MASK) {
+      if (!same) {
+        __syncthreads();                                   // (the last block's list has been read)
+        for (int i = wave; i < blk.nt; i += 4) {
+          const int key = (blk.lo + i) * 64 + lane;
+          const unsigned long long bits = __builtin_amdgcn_ballot_w64(key < blk.n0 && p.mask[(long long)blk.b * p.seg[0].n + key] != 0);
+          if (lane == 0) words[i] = bits;
+        }
+        __syncthreads();
+        // the tiles with a key move to the front (wave 0; every chunk is read before it is written, in front of itself)
+        if (wave == 0) {
+          int at = 0;
+          for (int i = 0; i < blk.nt; i += 64) {
+            const unsigned long long bits = i + lane < blk.nt ? words[i + lane] : 0ULL;
+            const unsigned long long some = __builtin_amdgcn_ballot_w64(bits != 0);
+            const int to = at + __popcll(some & low_bits(lane));
+            if (bits) { words[to] = bits; list[to] = (unsigned short)(i + lane); }
+            at += __popcll(some);
+          }
+          if (lane == 0) *(int*)(list + kListTiles) = at;
+        }
+        __syncthreads();
+        listed = __builtin_amdgcn_readfirstlane(*(volatile int*)(list + kListTiles));
+      }
+      same = more && after.b == blk.b && after.lo == blk.lo && after.nt == blk.nt;
+    }
+    const int nt = MASK ? listed : blk.nt, ant = MASK ? listed : after.nt;
+    // The next block's first tiles follow this one's last (of which a block that was itself begun ahead has three at least: the slots behind a
+    // shorter one hold its last tile again)
+    const bool ahead = more && nt > 0 && ant > 0 && (!MASK || same) && (!primed || nt >= 3);
+    const int lo = blk.lo, n0 = blk.n0, n1 = p.seg[1].n, tiles0 = blk.tiles0, b = blk.b, kh = blk.kh, row0 = blk.row0;
+    const bool whole = blk.whole, idle = row0 >= p.rows;
+    const unsigned int slot = 2 * w + (lo == 0 ? 1 : 0);
 #pragma unroll
-  for (int i = 0; i < DB; ++i)
+    for (int n = 0; n < QB; ++n)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = -1e30f, l = 0.f;
-  const int tri = lane & 15;
+      for (int s = 0; s < KS; ++s) {
+        qreg[n][s] = qnext[n][s];
+        asm volatile("" : "+v"(qreg[n][s]));               // Q has arrived: the loop does not wait for it, with the direct loads
+      }
 
-  if (nt > 0) {
-    load(0, 0);
-    load(nt > 1 ? 1 : 0, 1);
-    for (int i = 0, slot = 0; i < nt; ++i, slot = slot == 2 ? 0 : slot + 1) {
-      // tile i has landed for every wave, and every wave has read tile i - 1, whose slot takes tile i + 2
-      __builtin_amdgcn_s_waitcnt(((2 * LPT) & 0xF) | (((2 * LPT) >> 4) << 14) | (0x7 << 4) | (0 << 8));
-      block_sync();
-      load(i + 2 < nt ? i + 2 : nt - 1, slot == 0 ? 2 : slot - 1);
-      if (idle) continue;
-      const char* kt = smem + slot * 2 * TILE;
-      const char* vt = kt + TILE;
-      f32x16 s[2];
+    // Tile i of the list and which of its keys count.  Past the end: the next block's, or the last one again, which keeps the counts of loads in
+    // flight uniform.
+    struct Info { int t; bool next; unsigned long long w; };
+    auto info = [&](int i) DF_INLINE {
+      Info r;
+      r.next = i >= nt && ahead;
+      if (i >= nt) i = !ahead ? nt - 1 : i - nt < ant ? i - nt : ant - 1;
+      if constexpr (MASK) {
+        const unsigned long long bits = words[i];
+        r.t = lo + __builtin_amdgcn_readfirstlane((int)list[i]);
+        r.w = (unsigned long long)(unsigned int)__builtin_amdgcn_readfirstlane((int)bits) |
+              (unsigned long long)(unsigned int)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32;
+      } else {
+        const int z0 = r.next ? after.tiles0 : tiles0;
+        r.t = (r.next ? after.lo : lo) + i;
+        r.w = r.t < z0 ? low_bits((r.next ? after.n0 : n0) - r.t * 64) : low_bits(n1 - (r.t - z0) * 64);
+      }
+      return r;
+    };
+    // Where the wave's loads of a tile come from.  Keys that are none are read as one that is: their weight is 0, the value must be finite where
+    // the others are.
+    struct Source { const char* base; unsigned int ofs[LPT]; };
+    auto source = [&](auto isv, const Info& i) DF_INLINE {
+      constexpr bool V = decltype(isv)::value;
+      const int z0 = i.next ? after.tiles0 : tiles0;
+      const bool second = !MASK && i.t >= z0;
+      const Seg& s = p.seg[second ? 1 : 0];
+      const int ld = (int)(V ? s.ldv : s.ldk);
+      Source r;
+      r.base = (const char*)((const bf16_t*)(V ? s.v : s.k) + (long long)(i.next ? after.b : b) * (V ? s.bsv : s.bsk) +
+                             (long long)(i.next ? after.kh : kh) * (V ? s.hsv : s.hsk) + (long long)(second ? i.t - z0 : i.t) * 64 * ld);
+      const bool full = i.w == ~0ULL;
+      const int some = __builtin_ctzll(i.w);
+      const unsigned int mine = (unsigned int)(i.w >> (16 * wave));       // (a wave's loads cover 16 rows of the tile)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int j = 0; j < LPT; ++j) {
+        const int from = full || (mine >> (trow[j] & 15) & 1) ? trow[j] : some;
+        r.ofs[j] = 2u * (unsigned int)(from * ld) + (V ? vch[j] : kch[j]);
+        asm volatile("" : "+v"(r.ofs[j]));
+      }
+      return r;
+    };
+    auto load = [&](const Source& f, int j, int to) DF_INLINE { lds_load16(f.base, f.ofs[j], smem + to + 1024 * j); };
+    using IsK = std::false_type;
+    using IsV = std::true_type;
+
+    f32x16 o[QB][DB], sa[QB][2];
+    u32x4 pk[QB][4];
+    float m[QB], l[QB];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+    for (int n = 0; n < QB; ++n) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const int r = 32 * kb + csig;
-          const u32x4 a = *reinterpret_cast<const u32x4*>(kt + r * (D * 2) + (((2 * ks + g) ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 16));
-          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qreg[ks], s[kb], 0, 0, 0);
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[n][i][e] = 0.f;
+      m[n] = kLow; l[n] = 0.f;
+    }
+    // MASK: where the scores start, 0 or, for a key that is none, -infinity: 64 floats per tile, a slot beside its K
+    float* const bias = (float*)((char*)list + kListTiles * 2 + 16);
+    f32x16 start[2];
+    auto fetch_start = [&](int at, int kb) DF_INLINE {
+      if constexpr (MASK) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>((char*)bias + at / TILE * 256 + (32 * kb + 16 * (i >> 1) + 8 * g + 4 * (i & 1)) * 4);
+          start[kb][4 * i] = v.x; start[kb][4 * i + 1] = v.y; start[kb][4 * i + 2] = v.z; start[kb][4 * i + 3] = v.w;
         }
       }
-      const unsigned long long w = word_of(i, lo + tile_of(i));
-      if (w != ~0ULL) {
+    };
+    auto put_start = [&](int i, unsigned long long bits) DF_INLINE {       // by one wave, two barriers before it is read
+      if (MASK && wave == (i & 3)) bias[((s0 + i) & 3) * 64 + lane] = (bits >> lane) & 1 ? 0.f : -INFINITY;
+    };
+    auto s_mfma = [&](u32x4 k, int s, int kb, int n) DF_INLINE {
+      if (s == 0) {
+        if constexpr (MASK) {
+          sa[n][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), qreg[n][s], start[kb], 0, 0, 0);
+          return;
+        }
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!((w >> (32 * kb + 16 * (e >> 3) + 8 * g + (e & 7))) & 1)) s[kb][e] = -INFINITY;
+        for (int e = 0; e < 16; ++e) sa[n][kb][e] = 0.f;
       }
+      sa[n][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), qreg[n][s], sa[n][kb], 0, 0, 0);
+    };
+    auto pv_mfma = [&](u32x4 v, int ts, int db, int n) DF_INLINE {
+      o[n][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pk[n][ts]), o[n][db], 0, 0, 0);
+    };
+    auto scores = [&](int i) DF_INLINE {
+      const int kt = slot_of(s0 + i);
+      fetch_start(kt, 0);
+      fetch_start(kt, 1);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const u32x4 k = kfrag(kt, s, kb);
+#pragma unroll
+          for (int n = 0; n < QB; ++n) s_mfma(k, s, kb, n);
+        }
+    };
+    auto hide = [&](unsigned long long bits) DF_INLINE {             // scores of keys that are none
+      if (MASK || bits == ~0ULL) return;
+      const unsigned long long mine = bits >> (8 * g);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const bool off = !((mine >> (32 * kb + 16 * (e >> 3) + (e & 7))) & 1);
+#pragma unroll
+          for (int n = 0; n < QB; ++n)
+            if (off) sa[n][kb][e] = -INFINITY;
+        }
+    };
+    auto scale_by = [&](int n, float f) DF_INLINE {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[n][db][e] *= f;
+      l[n] *= f;
+    };
+    auto settle = [&](int n) DF_INLINE {                             // the maximum that covers the scores in sa too; the factor for what came before
+      float top = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, sa[n][kb][e]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * p.sc;
+      const float mn = fmaxf(m[n], top), alpha = __builtin_amdgcn_exp2f(m[n] - mn);
+      m[n] = mn;
+      return alpha;
+    };
+
+    // Iteration t: weights of tile t from the scores in sa, O += V P of tile t - 1 (PV), S of tile t + 1.  Sixteen slots of M * QB matrix
+    // instructions and their share of the vector instructions; operands are read from LDS some slots ahead.
+    Info cur, n1i, n2i, n3i;
+    Source ka, va;                                         // of K_{t+3} and V_{t+1}
+    float tsum[QB];
+    int x = 0;                                             // slot of tile t + 1; tile t - 1's, which tile t + 3 takes, is two from it
+    auto tile = [&](auto pvc) DF_INLINE {
+      constexpr bool PV = decltype(pvc)::value;
+      constexpr int A = M == 1 ? 4 : 3;
+      //                          slot: 0  1  2  3  4  5  6  7  8  9 10 11 12 13 14 15; of S (kb, quarter), of O (key step, half)
+      constexpr int kIsS[16] =       {0, 0, 0, 0, 0, 0, 1, 0, 1, 0, 1, 1, 1, 1, 1, 1};
+      constexpr int kFirst[16] =     {0, 0, 1, 1, 2, 2, 0, 3, 0, 3, 0, 0, 1, 1, 1, 1};
+      constexpr int kSecond[16] =    {0, 1, 0, 1, 0, 1, 0, 0, 1, 1, 2, 3, 0, 1, 2, 3};
+      const int kt = x, vt = x ^ (2 * TILE), kd = (x ^ (2 * TILE)) + wofs, vd = VR + x + wofs;
+      u32x4 f[16][M];
+      float ex[QB][2][8];
+      auto fetch = [&](int i) DF_INLINE {
+#pragma unroll
+        for (int k = 0; k < M; ++k) {
+          if (kIsS[i]) f[i][k] = kfrag(kt, kSecond[i] * M + k, kFirst[i]);
+          else if (PV) f[i][k] = vfrag(vt, kFirst[i], kSecond[i] * M + k);
+        }
+      };
+      auto E = [&](int u, int h) DF_INLINE {                         // four exponentials of key step u
+#pragma unroll
+        for (int n = 0; n < QB; ++n)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) ex[n][u & 1][4 * h + q] = __builtin_amdgcn_exp2f(fmaf(sa[n][u >> 1][8 * (u & 1) + 4 * h + q], p.sc, -m[n]));
+      };
+      auto C = [&](int u) DF_INLINE {                                // packing, behind the matrix instructions that read the old pk[u]
+#pragma unroll
+        for (int n = 0; n < QB; ++n) {
+          const float* x = ex[n][u & 1];
+          pk[n][u] = u32x4{pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3]), pack_bf2(x[4], x[5]), pack_bf2(x[6], x[7])};
+          asm volatile("" : "+v"(pk[n][u]));
+        }
+      };
+      auto S = [&](int u) DF_INLINE {                                // row sums
+#pragma unroll
+        for (int n = 0; n < QB; ++n) {
+          const float* x = ex[n][u & 1];
+          const float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+          tsum[n] = u == 0 ? s : tsum[n] + s;
+          asm volatile("" : "+v"(tsum[n]));
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < A; ++i) fetch(i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int k = 0; k < M; ++k)
+#pragma unroll
+          for (int n = 0; n < QB; ++n) {
+            if (kIsS[i]) s_mfma(f[i][k], kSecond[i] * M + k, kFirst[i], n);
+            else if (PV) pv_mfma(f[i][k], kFirst[i], kSecond[i] * M + k, n);
+          }
+        if (i + A < 16) fetch(i + A);
+        switch (i) {
+          case 0: E(0, 0); break;
+          case 1: E(0, 1); load(ka, 0, kd); break;
+          case 2: C(0); load(ka, 1, kd); break;
+          case 3: E(1, 0); fetch_start(kt, 0); break;
+          case 4: E(1, 1); break;
+          case 5: C(1); S(0); break;
+          case 6: E(2, 0); if constexpr (LPT > 2) load(ka, 2, kd); break;
+          case 7: E(2, 1); S(1); break;
+          case 8: C(2); load(va, 0, vd); break;
+          case 9: E(3, 0); fetch_start(kt, 1); break;
+          case 10: E(3, 1); load(va, 1, vd); break;
+          case 11: S(2); if constexpr (LPT > 2) load(ka, 3, kd); break;
+          case 12: C(3); if constexpr (LPT > 2) load(va, 2, vd); break;
+          case 13: S(3); break;
+          case 14: if constexpr (LPT > 2) load(va, 3, vd); break;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    constexpr float kMove = 0x1p13f, kRedo = 0x1p100f;
+    auto large = [&](int t) DF_INLINE {                              // a tile whose sums are far above 1 somewhere
+      bool redo = false;
+#pragma unroll
+      for (int n = 0; n < QB; ++n) redo |= __builtin_amdgcn_ballot_w64(tsum[n] > kRedo) != 0;
+      if (redo) {
+        scores(t);
+        hide(cur.w);
+#pragma unroll
+        for (int n = 0; n < QB; ++n) {
+          scale_by(n, settle(n));
+          tsum[n] = 0.f;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              x[e] = __builtin_amdgcn_exp2f(fmaf(sa[n][u >> 1][8 * (u & 1) + e], p.sc, -m[n]));
+              tsum[n] += x[e];
+            }
+            pk[n][u] = u32x4{pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3]), pack_bf2(x[4], x[5]), pack_bf2(x[6], x[7])};
+          }
+        }
+        scores(t + 1);
+        return;
+      }
+#pragma unroll
+      for (int n = 0; n < QB; ++n) {
+        const float both = fmaxf(tsum[n], __shfl_xor(tsum[n], 32, 64));
+        const int k = both > kMove ? __builtin_amdgcn_frexp_expf(both) : 0;
+        const float f = __builtin_amdgcn_ldexpf(1.0f, -k);
+        m[n] += (float)k;
+        scale_by(n, f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float a = __uint_as_float(pk[n][u][q] << 16) * f, z = __uint_as_float(pk[n][u][q] & 0xffff0000u) * f;
+            pk[n][u][q] = (__float_as_uint(a) >> 16) | (__float_as_uint(z) & 0xffff0000u);
+          }
+        tsum[n] *= f;
+      }
+    };
+
+    if (nt > 0) {
+      cur = info(0); n1i = info(1); n2i = info(2); n3i = info(3);
+      if (!primed) {
+        s0 = 0;
+        block_sync();                                      // (every wave's reads of the last block are done: they were waited for)
+        put_start(0, cur.w); put_start(1, n1i.w); put_start(2, n2i.w);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          ka = source(IsK{}, i == 0 ? cur : i == 1 ? n1i : n2i);
+#pragma unroll
+          for (int j = 0; j < LPT; ++j) load(ka, j, slot_of(i) + wofs);
+        }
+        va = source(IsV{}, cur);
+#pragma unroll
+        for (int j = 0; j < LPT; ++j) load(va, j, VR + wofs);
+        sync_tile();
+      }
+      auto next = [&](int t) DF_INLINE { cur = n1i; n1i = n2i; n2i = n3i; n3i = info(t + 4); };
+      // an iteration's loads, the starts of the scores of tile t + 3, and at the last one the next block's Q
+      auto begin = [&](int t) DF_INLINE {
+        ka = source(IsK{}, n3i);
+        va = source(IsV{}, n1i);
+        put_start(t + 3, n3i.w);
+        if (t == nt - 1 && ahead) queries(after);
+      };
+      if (idle) {
+        for (int t = 0; t < nt; ++t) {
+          begin(t);
+#pragma unroll
+          for (int j = 0; j < LPT; ++j) load(ka, j, slot_of(s0 + t + 3) + wofs);
+#pragma unroll
+          for (int j = 0; j < LPT; ++j) load(va, j, VR + slot_of(s0 + t + 1) + wofs);
+          next(t);
+          sync_tile();
+        }
+      } else {
+        auto finish = [&](int t) DF_INLINE {               // of an iteration
+          float most = tsum[0];
+          if constexpr (QB == 2) most = fmaxf(most, tsum[1]);
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(most > kMove) != 0, 0)) large(t);
+#pragma unroll
+          for (int n = 0; n < QB; ++n) l[n] += tsum[n];
+          x = (x + TILE) & (3 * TILE);
+          sync_tile();
+        };
+        scores(0);
+        hide(cur.w);
+#pragma unroll
+        for (int n = 0; n < QB; ++n) settle(n);
+        begin(0);
+        x = slot_of(s0 + 1);
+        tile(std::false_type{});
+#pragma unroll
+        for (int n = 0; n < QB; ++n) l[n] += tsum[n];      // (weights of at most 1)
+        x = slot_of(s0 + 2);
+        next(0);
+        sync_tile();
+        int t = 1;
+        while (t < nt) {
+          if constexpr (!MASK) {
+            // tiles t .. t + 3 whole and of one segment: as long as that holds
+            const int at = lo + t, second = at >= tiles0;
+            int run = (second ? tiles0 + (n1 >> 6) : n0 >> 6) - lo;
+            if (run > nt) run = nt;
+            if (t + 3 < run) {
+              const Seg& s = p.seg[second];
+              const long long kstep = 128 * s.ldk, vstep = 128 * s.ldv;
+              ka = source(IsK{}, info(t + 3));
+              va = source(IsV{}, info(t + 1));
+              cur.w = ~0ULL;
+              do {
+                tile(std::true_type{});
+                ka.base += kstep;
+                va.base += vstep;
+                finish(t);
+                ++t;
+              } while (t + 3 < run);
+              cur = info(t); n1i = info(t + 1); n2i = info(t + 2); n3i = info(t + 3);
+              continue;
+            }
+          }
+          begin(t);
+          hide(cur.w);
+          tile(std::true_type{});
+          finish(t);
+          next(t);
+          ++t;
+        }
+        const int vt = slot_of(s0 + nt - 1);
+#pragma unroll
+        for (int ts = 0; ts < 4; ++ts)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const u32x4 v = vfrag(vt, ts, db);
+#pragma unroll
+            for (int n = 0; n < QB; ++n) pv_mfma(v, ts, db, n);
+          }
+      }
+      // V has been read; no direct load outlives the wave, or its slot's part in the ring where the next block starts one of its own
+      if (ahead) __builtin_amdgcn_s_waitcnt(0xc07f);
+      else __builtin_amdgcn_s_waitcnt(0x0070);
+      s0 = (s0 + nt) & 3;
+    }
+    primed = ahead;
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+      if (row0 + 32 * n + c >= p.rows) continue;
+      const float lt = l[n] + __shfl_xor(l[n], 32, 64);
+      const float inv = !whole ? 1.f : nt > 0 ? 1.0f / lt : 0.f;          // no key: zeros (all scores -inf: 0 / 0, as the formula)
+      const int at0 = wave * 32 * QB + 32 * n + c;
+      bf16_t* op = (bf16_t*)p.out + row_offset(p, b, kh, row0 + 32 * n + c, (long long)p.Lq * p.kv_heads * p.group * p.d, (long long)p.kv_heads * p.group * p.d);
+      float* po = p.part_o + ((long long)slot * BLK + at0) * p.d;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const int at = 32 * db + 16 * f + 8 * g;
+          if (at >= p.d) continue;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = o[n][db][8 * f + e] * inv;
+          if (whole) {
+            st_vec(op + at, v);
+          } else {
+            st_vec(po + at, v);
+            st_vec(po + at + 4, v + 4);
+          }
+        }
+      if (!whole && g == 0) {
+        float* ml = p.part_ml + 2 * ((long long)slot * BLK + at0);
+        ml[0] = nt > 0 ? m[n] : -INFINITY;
+        ml[1] = lt;
+      }
+    }
+    blk = after;
+  }
+}
+
+// n parts of a row, in order, eight values of it from `at` on; part i lies in row where(i).  Four at a time are requested at once: one after the other
+// each waits for memory.
+template <typename F>
+__device__ __forceinline__ void merge_parts(const QParams& p, int n, int at, F where, float& m, float& l, float (&o)[8]) {
+  for (int i0 = 0; i0 < n; i0 += 4) {
+    f32x2 ml[4];
+    float v[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long r = where(i0 + i < n ? i0 + i : n - 1);
+      ml[i] = *reinterpret_cast<const f32x2*>(p.part_ml + 2 * r);
+      ld_vec(p.part_o + r * p.d + at, v[i]);
+      ld_vec(p.part_o + r * p.d + at + 4, v[i] + 4);
+    }
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mn = fmaxf(mn, ml[i].x);   // (the last one again where there are fewer: no other maximum)
+    if (mn == -INFINITY) continue;
+    const float f = __builtin_amdgcn_exp2f(m - mn);        // 0 at first
+    m = mn;
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] *= f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i0 + i >= n || ml[i].x == -INFINITY) continue;   // (a part without keys)
+      const float w = __builtin_amdgcn_exp2f(ml[i].x - m);
+      l = fmaf(w, ml[i].y, l);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(w, v[i][e], o[e]);
+    }
+  }
+}
+
+// The parts of a block that shares cut: its first share's (slot 2 w + 1), then those of the shares that begin inside it (slot 2 w), in that order.
+// Eight values of a row per lane.
+__global__ __launch_bounds__(256) void merge_shares(QParams p, Share sh, int blk, unsigned int per_row) {
+  const unsigned int nrb = (unsigned int)(p.rows + blk - 1) / blk, block = blockIdx.x;
+  const unsigned int w0 = share_of(sh, block * sh.tiles), w1 = share_of(sh, block * sh.tiles + sh.tiles - 1);
+  if (w0 == w1) return;
+  const unsigned int idx = blockIdx.y * 256 + threadIdx.x;
+  const int r = (int)(idx / per_row), at = (int)(idx - r * per_row) * 8;
+  const int bh = (int)(block / nrb), b = bh / p.kv_heads, kh = bh - b * p.kv_heads, row = (int)(block % nrb) * blk + r;
+  if (r >= blk || row >= p.rows) return;
+  float m = -INFINITY, l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  merge_parts(p, (int)(w1 - w0 + 1), at, [&](int i) DF_INLINE { return (long long)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * blk + r; }, m, l, o);
+  const float inv = m == -INFINITY ? 0.f : 1.0f / l;       // no key in any part: zeros
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] *= inv;
+  const long long ld = (long long)p.kv_heads * p.group * p.d;
+  st_vec((bf16_t*)p.out + row_offset(p, b, kh, row, (long long)p.Lq * ld, ld) + at, o);
+}
+
+// ---- few keys ----
+// The keys of a split, at most kHeldBytes of them, are brought to LDS once (every load in flight at a time) and stay there; each wave then takes
+// blocks of 32 rows on its own, without barriers.  For short prompts, for patches whose keys are few, and, with the keys split over workgroups, for
+// few rows against more keys.  KV4: segment 0 is the 4-bit cache itself, converted on its way to LDS (levels times scale is exact in bf16), V
+// transposed as it is held; the patch's own rows of it are no keys.
+constexpr int kHeldBytes = 128 * 1024;
+template <int D, int NW, bool MASK, bool KV4>
+__global__ __launch_bounds__(64 * NW, 2) void held_attn(QParams p, int row_groups, int own_tiles) {
+  constexpr int TILE = 64 * D * 2, CH = D / 8, KS = D / 16, DB = D / 32, RPI = 1024 / (D * 2), NI = TILE / 1024;
+  extern __shared__ __attribute__((aligned(16))) char smem[];             // K and V tile of each; where their scores start; their words
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, c = lane & 31, csig = (c & 0x13) | ((c & 4) << 1) | ((c & 8) >> 1), tri = lane & 15;
+  int rg, kh, b, split;
+  place(p, row_groups, rg, kh, b, split);
+  const int n0 = seg0_rows(p, b), n1 = p.seg[1].n;
+  // tiles of segment 0 (without the `own_tiles` in the middle that hold nothing but the patch's rows), then of segment 1
+  const int first_own = (p.own_lo + 63) >> 6, tiles0 = ((n0 + 63) >> 6) - own_tiles, all = tiles0 + ((n1 + 63) >> 6);
+  const int lo = split * p.tiles_per_split, hi = lo + p.tiles_per_split < all ? lo + p.tiles_per_split : all, nt = hi > lo ? hi - lo : 0;
+  float* const start = (float*)(smem + 2 * TILE * p.tiles_per_split);
+  unsigned long long* const words = (unsigned long long*)(start + 64 * p.tiles_per_split);
+
+  auto queries = [&](int row0, u32x4 (&q)[KS]) DF_INLINE {
+    const bool have = row0 + c < p.rows;
+    const bf16_t* qp = (const bf16_t*)p.q + row_offset(p, b, kh, have ? row0 + c : 0, p.bsq, p.ldq);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      q[s] = u32x4{0u, 0u, 0u, 0u};
+      if (have && 16 * s + 8 * g < p.d) q[s] = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * g);
+    }
+  };
+  int row0 = (rg * NW + wave) * 32;
+  const int step = row_groups * NW * 32;
+  u32x4 q[KS];
+  if (row0 < p.rows) queries(row0, q);
+
+  // A wave takes whole tiles of K or V
+  for (int u = wave; u < 2 * nt; u += NW) {
+    const int i = u >> 1, isv = u & 1;
+    int t = lo + i;
+    const bool second = t >= tiles0;
+    t = second ? t - tiles0 : t < first_own ? t : t + own_tiles;
+    const int key = t * 64 + lane, n = second ? n1 : n0;
+    bool valid = key < n;
+    if (MASK && valid) valid = p.mask[(long long)b * p.seg[0].n + key] != 0;
+    if (KV4 && !second && p.own_n > 0) {
+      const int rel = (p.own_period > 0 ? key % p.own_period : key) - p.own_lo;
+      if (rel >= 0 && rel < p.own_n) valid = false;
+    }
+    const unsigned long long bits = __builtin_amdgcn_ballot_w64(valid);
+    if (!isv) {
+      start[64 * i + lane] = valid ? 0.f : -INFINITY;
+      if (lane == 0) words[i] = bits;
+    }
+    if (bits == 0) continue;
+    char* const to = smem + (2 * i + isv) * TILE;
+    if (!KV4 || second) {
+      const Seg& s = p.seg[second ? 1 : 0];
+      const long long ld = isv ? s.ldv : s.ldk;
+      const bf16_t* src = (const bf16_t*)(isv ? s.v : s.k) + (long long)b * (isv ? s.bsv : s.bsk) + (long long)kh * (isv ? s.hsv : s.hsk) + (long long)t * 64 * ld;
+      const int some = __builtin_ctzll(bits);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const int r = j * RPI + lane / CH, at = lane % CH;
+        const int kc = (at ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 8, vc = (at ^ (D == 64 ? ((r >> 1) & 1) * 2 ^ ((r >> 3) & 1) * 4 : (r & 3) * 4)) * 8;
+        const int ch = isv ? vc : kc, from = (bits >> r) & 1 ? r : some;
+        lds_load16(src + (long long)from * ld + (ch < p.d ? ch : 0), to + j * 1024);
+      }
+    } else {
+      const long long base = ((long long)b * p.kv_heads + kh) * p.c.pitch + (long long)t * 64;
+      if (!isv) {                                          // a key per lane
+        const float s = valid ? bf2f(p.c.ks[base + lane]) : 0.f;
+        const u32x4* src = reinterpret_cast<const u32x4*>(p.c.kc + (base + lane) * (D / 2));
+        u32x4 w[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) w[j] = src[j];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+          float x[8];
+          kv4_values(w[j >> 2][j & 3], s, x);
+          st_vec((bf16_t*)(to + lane * (D * 2) + ((j ^ (D == 64 ? (lane >> 1) & 7 : lane & 15)) * 16)), x);
+        }
+      } else {                                             // values of all keys: rows of V^T
+#pragma unroll
+        for (int e0 = 0; e0 < D; e0 += 8) {                // eight values, eight keys a lane
+          const int e = e0 + (lane >> 3), o = lane & 7;
+          const unsigned int w = *reinterpret_cast<const unsigned int*>(p.c.vc + (base >> 6) * (D * 32) + e * 32 + o * 4);
+          const u32x4 sv = *reinterpret_cast<const u32x4*>(p.c.vs + base + 8 * o);
+          const f32x2 a[4] = {kv4_levels<0>(w), kv4_levels<1>(w), kv4_levels<2>(w), kv4_levels<3>(w)};
+          float x[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float s = __uint_as_float(k & 1 ? sv[k >> 1] & 0xffff0000u : sv[k >> 1] << 16);
+            x[k] = (bits >> (8 * o + k)) & 1 ? a[k >> 1][k & 1] * s : 0.f;
+          }
+          st_vec((bf16_t*)(to + e * 128 + ((o ^ ((e >> 1) & 7)) * 16)), x);
+        }
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0070);                      // the wave's loads have landed
+  __syncthreads();
+
+  for (; row0 < p.rows; row0 += step) {
+    u32x4 qn[KS];
+    const bool more = row0 + step < p.rows;
+    if (more) queries(row0 + step, qn);
+    f32x16 o[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float m = kLow, l = 0.f;
+    bool any = false;
+    for (int i = 0; i < nt; ++i) {
+      if (MASK || KV4) {
+        const unsigned long long bits = words[i];
+        if (__builtin_amdgcn_readfirstlane((int)bits | (int)(bits >> 32)) == 0) continue;
+      }
+      any = true;
+      const char *kt = smem + 2 * i * TILE, *vt = kt + TILE;
+      f32x16 s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(start + 64 * i + 32 * kb + 16 * (j >> 1) + 8 * g + 4 * (j & 1));
+          s[kb][4 * j] = v.x; s[kb][4 * j + 1] = v.y; s[kb][4 * j + 2] = v.z; s[kb][4 * j + 3] = v.w;
+        }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const int r = 32 * kb + csig;
+          const u32x4 a = *reinterpret_cast<const u32x4*>(kt + r * (D * 2) + (((2 * ks + g) ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 16));
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, q[ks]), s[kb], 0, 0, 0);
+        }
       float top = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -210,64 +836,61 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_attn(QParams p) {
       for (int u = 0; u < 4; ++u) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + e], p.sc, -m));
-          l += x[e];
-        }
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + e], p.sc, -m));
+        l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
         pk[u] = u32x4{pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3]), pack_bf2(x[4], x[5]), pack_bf2(x[6], x[7])};
       }
+      if (KV4 && lo + i < tiles0) {                        // V^T as the cache holds it
 #pragma unroll
-      for (int ts = 0; ts < 4; ++ts)
+        for (int ts = 0; ts < 4; ++ts)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const int key = 16 * ts + 8 * g + (tri >> 2);
-          const int chunk = 4 * db + 2 * ((lane >> 4) & 1) + (tri & 1);
-          const int pc = D == 64 ? chunk ^ (2 * ((key >> 1) & 1)) ^ (4 * ((key >> 3) & 1)) : chunk ^ ((key & 3) * 4);
-          const char* at = vt + key * (D * 2) + pc * 16 + ((tri >> 1) & 1) * 8;
-          typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-          const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at));
-          // keys 4 .. 7 of the eight; their swizzle (by key & 3 or by bits 1 and 3) is the same
-          const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at + 4 * D * 2));
-          const bf16x8 a = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, pk[ts]), o[db], 0, 0, 0);
-        }
+          for (int db = 0; db < DB; ++db) {
+            const int r = 32 * db + csig;
+            const u32x4 a = *reinterpret_cast<const u32x4*>(vt + r * 128 + (((2 * ts + g) ^ ((r >> 1) & 7)) * 16));
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, pk[ts]), o[db], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int ts = 0; ts < 4; ++ts)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const int key = 16 * ts + 8 * g + (tri >> 2), chunk = 4 * db + 2 * ((lane >> 4) & 1) + (tri & 1);
+            const int pc = D == 64 ? chunk ^ (2 * ((key >> 1) & 1)) ^ (4 * ((key >> 3) & 1)) : chunk ^ ((key & 3) * 4);
+            const char* at = vt + key * (D * 2) + pc * 16 + ((tri >> 1) & 1) * 8;
+            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+            const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at));
+            const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at + 4 * D * 2));
+            const bf16x8 a = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, pk[ts]), o[db], 0, 0, 0);
+          }
+      }
     }
-    __builtin_amdgcn_s_waitcnt(0xf70);         // no direct load outlives the wave
     l += __shfl_xor(l, 32, 64);
-    if (l == 0.f) l = __uint_as_float(0x7fc00000u);        // keys, and every score -inf: no softmax
-  } else {
-    m = -INFINITY;
-  }
-  if (!have) return;
-  if (p.nsplit == 1) {
-    const float inv = nt > 0 ? 1.0f / l : 0.f;             // no key: zeros
-    bf16_t* op = (bf16_t*)p.out + row_offset(p, b, kh, row, (long long)p.Lq * p.kv_heads * p.group * p.d, (long long)p.kv_heads * p.group * p.d);
+    const int row = row0 + c;
+    if (row < p.rows) {
+      const float inv = p.nsplit > 1 ? 1.f : any ? 1.0f / l : 0.f;        // no key: zeros
+      bf16_t* op = (bf16_t*)p.out + row_offset(p, b, kh, row, (long long)p.Lq * p.kv_heads * p.group * p.d, (long long)p.kv_heads * p.group * p.d);
+      const long long at0 = ((long long)split * p.B * p.kv_heads + (long long)b * p.kv_heads + kh) * p.rows + row;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int at = 32 * db + 16 * f + 8 * g;
-        if (at >= p.d) continue;
-        float v[8];
+        for (int f = 0; f < 2; ++f) {
+          const int at = 32 * db + 16 * f + 8 * g;
+          if (at >= p.d) continue;
+          float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = o[db][8 * f + e] * inv;
-        st_vec(op + at, v);
-      }
-  } else {
-    const long long at0 = ((long long)split * p.B * p.kv_heads + (long long)b * p.kv_heads + kh) * p.rows + row;
+          for (int e = 0; e < 8; ++e) v[e] = o[db][8 * f + e] * inv;
+          if (p.nsplit == 1) {
+            st_vec(op + at, v);
+          } else {
+            st_vec(p.part_o + at0 * p.d + at, v);
+            st_vec(p.part_o + at0 * p.d + at + 4, v + 4);
+          }
+        }
+      if (p.nsplit > 1 && g == 0) { p.part_ml[2 * at0] = any ? m : -INFINITY; p.part_ml[2 * at0 + 1] = l; }
+    }
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int at = 32 * db + 16 * f + 8 * g;
-        if (at >= p.d) continue;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = o[db][8 * f + e];
-        st_vec(p.part_o + at0 * p.d + at, v);
-        st_vec(p.part_o + at0 * p.d + at + 4, v + 4);
-      }
-    if (g == 0) { p.part_ml[2 * at0] = m; p.part_ml[2 * at0 + 1] = l; }
+    for (int s = 0; s < KS; ++s) q[s] = qn[s];
   }
 }
 
@@ -282,18 +905,7 @@ __global__ __launch_bounds__(256) void merge_splits(QParams p, unsigned int per_
   const int at = (int)(idx - row * per_row) * 8;
   const unsigned int all = (unsigned int)(p.B * p.kv_heads) * (unsigned int)p.rows;
   float m = -INFINITY, l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < p.nsplit; ++s) m = fmaxf(m, p.part_ml[2 * ((long long)s * all + row)]);
-  for (int s = 0; s < p.nsplit; ++s) {
-    const long long r = (long long)s * all + row;
-    const float ms = p.part_ml[2 * r], w = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - m);
-    float v[8];
-    ld_vec(p.part_o + r * p.d + at, v);
-    ld_vec(p.part_o + r * p.d + at + 4, v + 4);
-    if (ms == -INFINITY) continue;
-    l = fmaf(w, p.part_ml[2 * r + 1], l);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = fmaf(w, v[e], o[e]);
-  }
+  merge_parts(p, p.nsplit, at, [&](int s) DF_INLINE { return (long long)s * all + row; }, m, l, o);
   const float inv = m == -INFINITY ? 0.f : 1.0f / l;       // no key in any split: zeros
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] *= inv;
@@ -333,7 +945,7 @@ __global__ __launch_bounds__(256) void float_attn(QParams p) {
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = -1e30f, l = 0.f;
+  float m = kLow, l = 0.f;
   bool any = false;                                        // a key so far
   for (int t = lo; t < hi; ++t) {
     const bool second = t >= tiles0;
@@ -424,7 +1036,6 @@ __global__ __launch_bounds__(256) void float_attn(QParams p) {
     }
   }
   l += __shfl_xor(l, 32, 64);
-  if (any && l == 0.f) l = __uint_as_float(0x7fc00000u);
   if (!any) m = -INFINITY;
   if (!have) return;
   const long long at0 = ((long long)split * p.B * p.kv_heads + (long long)b * p.kv_heads + kh) * p.rows + row;
@@ -504,7 +1115,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kv4(QParams p) {
   for (int n = 0; n < NQ; ++n) {
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m[n] = -1e30f; l[n] = 0.f;
+    m[n] = kLow; l[n] = 0.f;
   }
   const bool any = lo + wave < hi;
   Tile cur, nxt;
@@ -581,7 +1192,6 @@ __global__ __launch_bounds__(256, 2) void few_rows_kv4(QParams p) {
   for (int n = 0; n < NQ; ++n) {
     float ln = l[n] + __shfl_xor(l[n], 16, 64);
     ln += __shfl_xor(ln, 32, 64);
-    if (any && ln == 0.f) ln = __uint_as_float(0x7fc00000u);
     if (n) __syncthreads();
 #pragma unroll
     for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(red + (wave * 16 + rho) * ROW + 16 * db + 4 * gg) = o[n][db];
@@ -615,63 +1225,201 @@ __global__ __launch_bounds__(256, 2) void few_rows_kv4(QParams p) {
 }
 
 // ---- choice of kernel and splits, all from the arguments' sizes ----
-enum { kRows, kFewKv4, kFloat };
+enum { kRows, kHeld, kFewKv4, kFloat };
 struct Plan {
-  int kind, nq;                                // nq: blocks of 16 rows (kFewKv4)
+  int kind, nq;                                // nq: blocks of 16 (kFewKv4) or of 32 rows a wave (kRows), waves (kHeld)
   int block, tile;                             // rows of a workgroup, keys of a tile
-  int nsplit, tiles_per_split;
-  size_t expand, parts;                        // bytes of the workspace: the cache's rows in bf16, the splits' parts
+  int nsplit, tiles_per_split;                 // all but kRows
+  int row_groups, own_tiles;                   // kHeld
+  Share share;                                 // kRows
+  bool ok;
+  size_t expand, parts;                        // bytes of the workspace: the cache's rows in bf16, the parts of the splits or shares
 };
 
-// `keys`: of both segments; `cached`: segment 0 is a 4-bit cache of whose rows `other` are not the patch's
-Plan plan_of(int B, long long rows, int kv_heads, int d, long long keys0, long long keys1, bool cached, bool masked, int dtype) {
-  Plan r = {};
-  const long long heads = (long long)B * kv_heads;
-  if (dtype == DF_F32) { r.kind = kFloat; r.block = 128; r.tile = 32; }
-  else if (cached && keys1 == 0 && rows <= 64) { r.kind = kFewKv4; r.nq = rows > 16 ? 2 : 1; r.block = 16 * r.nq; r.tile = 64; }
-  else { r.kind = kRows; r.block = d <= 64 ? 128 : 256; r.tile = 64; }
-  const long long tiles = (keys0 + r.tile - 1) / r.tile + (keys1 + r.tile - 1) / r.tile;
-  const long long blocks = heads * ((rows + r.block - 1) / r.block);
-  long long ns = 1;
-  const long long want = r.kind == kFewKv4 ? 768 : r.kind == kRows && d > 64 ? 256 : 512, least = r.kind == kFewKv4 ? 4 : 4;
-  if (blocks < want) ns = want / blocks;
-  if (ns > tiles / least) ns = tiles / least;
-  if (ns < 1) ns = 1;
-  if (ns > 64) ns = 64;
-  if (masked && r.kind == kRows && ns < (tiles + kListTiles - 1) / kListTiles) ns = (tiles + kListTiles - 1) / kListTiles;
+// What an attention is to be planned for: `own` of `L` keys are fresh rows beside a cache, in a row from own_lo on (or not: own_period)
+struct Task {
+  int B, kv_heads, d, dtype;
+  long long rows, L, own, own_lo;
+  bool cached, masked, period;
+};
+
+// Microseconds of writing and merging `parts` rows of partial results
+double merge_us(double parts, int d) { return 3.3 + parts * (d + 2) * 8.0 / 3.5e6; }
+
+// The held form with `ns` splits and `nw` waves: its plan, and its predicted microseconds.  A wave takes 0.7 us for 32 rows and a tile of 64 keys of 64
+// values where it has its SIMD to itself, two 1.2; 128 values 1.15 and 2.1; a tile of codes 0.3 more to convert.
+double plan_held(const Task& k, long long ns, int nw, Plan& r) {
+  r = Plan{};
+  r.ok = true;
+  const long long heads = (long long)k.B * k.kv_heads;
+  const int D = k.d <= 64 ? 64 : 128, held = 2 * 64 * D * 2, most = kHeldBytes / held;
+  r.kind = kHeld; r.tile = 64;
+  if (k.cached && k.own > 0 && !k.period) {
+    const long long first = (k.own_lo + 63) / 64, last = (k.own_lo + k.own) / 64;
+    if (last > first) r.own_tiles = (int)(last - first);
+  }
+  const long long tiles = (k.L + 63) / 64 - r.own_tiles + (k.cached ? (k.own + 63) / 64 : 0), blocks = (k.rows + 31) / 32;
   r.tiles_per_split = (int)((tiles + ns - 1) / ns);
+  if (r.tiles_per_split > most) return 1e30;
   r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
-  if (cached && r.kind == kRows) r.expand = (size_t)(heads * keys0 * d * 4 + 255) / 256 * 256;
-  if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * rows * (d + 2) * sizeof(float);
+  r.nq = nw;
+  r.block = 32 * nw;
+  const long long groups = (blocks + nw - 1) / nw, by_lds = 160 * 1024 / (r.tiles_per_split * (held + 264)), cap = by_lds < 8 / nw ? by_lds : 8 / nw;
+  const long long fit = 256 * cap / (heads * r.nsplit);                    // workgroups along the rows for one round
+  const long long each = fit < 1 ? groups : (groups + fit - 1) / fit;      // blocks of a wave
+  r.row_groups = (int)((groups + each - 1) / each);
+  const long long wgs = r.row_groups * heads * r.nsplit, rounds = (wgs + 256 * cap - 1) / (256 * cap);
+  if (wgs > 0x7fffffffLL) return 1e30;
+  const long long on_cu = rounds > 1 ? cap : (wgs + 255) / 256;
+  const bool two = on_cu * nw > 4;
+  const double tile = D == 64 ? (two ? 1.2 : 0.7) : (two ? 2.1 : 1.15);
+  if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * k.rows * (k.d + 2) * sizeof(float);
+  return 3.6 + (D == 64 ? 0.0 : 0.5) + (double)(rounds * each) * r.tiles_per_split * tile + (k.cached ? 0.3 * (double)rounds * r.tiles_per_split : 0.0) +
+         (r.nsplit > 1 ? merge_us((double)r.nsplit * heads * k.rows, k.d) : 0.0);
+}
+
+// The pipelined form with `qb` blocks of 32 rows a wave.  A tile takes a workgroup 0.85 us, two on a unit 1.16 (128 values 1.1; 256 rows 1.05, one on a
+// unit); its code is long, the first pass over it costs.
+double plan_rows(const Task& k, int qb, Plan& r) {
+  r = Plan{};
+  r.ok = true;
+  const long long heads = (long long)k.B * k.kv_heads, keys0 = k.cached ? k.L - k.own : k.L, keys1 = k.cached ? k.own : 0;
+  r.kind = kRows; r.nq = qb; r.block = 128 * qb; r.tile = 64;
+  const long long tiles = (keys0 + 63) / 64 + (keys1 + 63) / 64, blocks = heads * ((k.rows + r.block - 1) / r.block), all = blocks * tiles;
+  if (k.cached) r.expand = (size_t)(heads * keys0 * k.d * 4 + 255) / 256 * 256;
+  // Whole blocks, the same number each, where that takes hardly longer than cutting the line into as many equal shares as workgroups fit the chip
+  // (the parts and their merge cost about as much as kCut tiles); shares of four tiles or more.
+  constexpr long long kCut = 10;
+  const long long fit = k.d <= 64 && qb == 1 ? 512 : 256, rounds = (blocks + fit - 1) / fit;
+  r.ok = all < (1LL << 31) - (1LL << 20);
+  if (!r.ok) return 1e30;
+  Share& s = r.share;
+  s.tiles = (unsigned int)tiles; s.all = (unsigned int)all;
+  if (rounds * tiles <= (all + fit - 1) / fit + kCut && (!k.masked || tiles <= kListTiles)) {
+    s.per = (unsigned int)(rounds * tiles);
+    s.count = (unsigned int)((blocks + rounds - 1) / rounds);
+  } else {
+    long long n = all / 4 < fit ? all / 4 : fit;
+    if (k.masked && n < all / (kListTiles - 1) + 1) n = all / (kListTiles - 1) + 1;
+    if (n < 1) n = 1;
+    s.count = (unsigned int)n; s.per = (unsigned int)(all / n); s.more = (unsigned int)(all % n);
+    r.parts = (size_t)n * 2 * r.block * (k.d + 2) * sizeof(float);
+  }
+  const bool two = fit == 512 && s.count > 256;
+  const double tile = k.d > 64 ? 1.1 : qb == 2 ? 1.05 : two ? 1.16 : 0.85;
+  return (k.d > 64 || qb == 2 ? 7.7 : 6.2) + tile * (double)(s.per + 1) * (double)((s.count + fit - 1) / fit) +
+         (r.parts ? merge_us(1.2 * (double)s.count * r.block, k.d) : 0.0) + (k.cached ? 4.0 + (double)(heads * keys0) * k.d * 4.5 / 4e6 : 0.0);
+}
+
+Plan choose(const Task& k) {
+  Plan r = {};
+  r.ok = true;
+  const long long heads = (long long)k.B * k.kv_heads, rows = k.rows, own = k.cached ? k.own : 0;
+  if (k.dtype == DF_F32 || (k.cached && own == 0 && rows <= 64)) {
+    if (k.dtype == DF_F32) { r.kind = kFloat; r.block = 128; r.tile = 32; }
+    else { r.kind = kFewKv4; r.nq = rows > 16 ? 2 : 1; r.block = 16 * r.nq; r.tile = 64; }
+    const long long tiles = (k.L - own + r.tile - 1) / r.tile + (own + r.tile - 1) / r.tile, blocks = heads * ((rows + r.block - 1) / r.block);
+    long long ns = 1;
+    const long long want = r.kind == kFewKv4 ? 768 : 512;
+    if (blocks < want) ns = want / blocks;
+    if (ns > tiles / 4) ns = tiles / 4;
+    if (ns < 1) ns = 1;
+    if (ns > 64) ns = 64;
+    r.tiles_per_split = (int)((tiles + ns - 1) / ns);
+    r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
+    if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * rows * (k.d + 2) * sizeof(float);
+    return r;
+  }
+  // The form that is predicted to take least
+  double best = 1e30;
+  auto offer = [&](double us, const Plan& q) {
+    if (us < best - 1e-9) { best = us; r = q; }
+  };
+  Plan q;
+#ifdef DF_TUNING
+  const char* form = tune_env("DF_QATTN");
+  if (form && !strcmp(form, "rows1")) { plan_rows(k, 1, q); return q; }
+  if (form && !strcmp(form, "rows2")) { plan_rows(k, k.d <= 64 ? 2 : 1, q); return q; }
+#endif
+  const long long keys = (k.L + 63) / 64 + (own + 63) / 64;
+  for (int tps = k.d <= 64 ? 8 : 4; tps >= 1; --tps) {    // tiles that a workgroup holds
+    if (tps > keys && tps > 1) continue;
+    const long long ns = (keys + tps - 1) / tps;
+    if (ns > 48) break;
+    offer(plan_held(k, ns, 4, q), q);
+    if (rows > 128) offer(plan_held(k, ns, 8, q), q);
+  }
+#ifdef DF_TUNING
+  if (form && !strcmp(form, "held") && best < 1e29) return r;
+#endif
+  offer(plan_rows(k, 1, q), q);
+  if (k.d <= 64) offer(plan_rows(k, 2, q), q);
+  if (best >= 1e29) r.ok = false;
   return r;
 }
 
-template <int D, int NW>
-int launch_rows(const QParams& p, bool masked, dim3 grid, hipStream_t st) {
-  constexpr int smem = 6 * 64 * D * 2, list = kListTiles * 10 + 16;
+// The choice takes 1.5 us; a call asks twice (its workspace, then itself) and a program for the same sizes again and again, so a thread keeps its last.
+const Plan& plan_of(const Task& k) {
+  thread_local Task last = {};
+  thread_local Plan plan = {};
+  if (last.B != k.B || last.kv_heads != k.kv_heads || last.d != k.d || last.dtype != k.dtype || last.rows != k.rows || last.L != k.L || last.own != k.own ||
+      last.own_lo != k.own_lo || last.cached != k.cached || last.masked != k.masked || last.period != k.period || tune_env("DF_QATTN")) {
+    plan = choose(k);
+    last = k;
+  }
+  return plan;
+}
+
+template <int D, int QB>
+int launch_rows(const QParams& p, const Plan& r, bool masked, hipStream_t st) {
+  constexpr int smem = 8 * 64 * D * 2, list = kListTiles * 10 + 16 + 4 * 256;
   static const hipError_t set = [] {
-    const hipError_t e = hipFuncSetAttribute((const void*)rows_attn<D, NW, true>, hipFuncAttributeMaxDynamicSharedMemorySize, smem + list);
-    return e != hipSuccess ? e : hipFuncSetAttribute((const void*)rows_attn<D, NW, false>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const hipError_t e = hipFuncSetAttribute((const void*)rows_attn<D, QB, true>, hipFuncAttributeMaxDynamicSharedMemorySize, smem + list);
+    return e != hipSuccess ? e : hipFuncSetAttribute((const void*)rows_attn<D, QB, false>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
   }();
   if (set != hipSuccess) return DF_EHIP;
-  if (masked) hipLaunchKernelGGL((rows_attn<D, NW, true>), grid, dim3(64 * NW), smem + list, st, p);
-  else hipLaunchKernelGGL((rows_attn<D, NW, false>), grid, dim3(64 * NW), smem, st, p);
+  if (masked) hipLaunchKernelGGL((rows_attn<D, QB, true>), dim3(r.share.count), dim3(256), smem + list, st, p, r.share);
+  else hipLaunchKernelGGL((rows_attn<D, QB, false>), dim3(r.share.count), dim3(256), smem, st, p, r.share);
+  if (r.parts) {
+    DF_LAUNCH_CHECK();
+    const unsigned int per_row = (unsigned int)(p.d / 8), blocks = (unsigned int)((p.rows + r.block - 1) / r.block * (long long)p.kv_heads * p.B);
+    hipLaunchKernelGGL(merge_shares, dim3(blocks, (unsigned)((r.block * per_row + 255) / 256)), dim3(256), 0, st, p, r.share, r.block, per_row);
+  }
   return DF_OK;
 }
 
 }  // namespace
 
-size_t qattn_workspace(int B, long long rows, int kv_heads, int d, long long keys0, long long keys1, bool cached, bool masked, int dtype) {
-  const Plan r = plan_of(B, rows, kv_heads, d, keys0, keys1, cached, masked, dtype);
+size_t qattn_workspace(int B, long long rows, int kv_heads, int d, long long L, long long own, long long own_lo, bool period, bool cached, bool masked,
+                       int dtype) {
+  const Plan r = plan_of(Task{B, kv_heads, d, dtype, rows, L, own, own_lo, cached, masked, period});
   return r.expand + r.parts;
+}
+
+template <int D, int NW>
+int launch_held(const QParams& p, const Plan& r, bool masked, bool cached, hipStream_t st) {
+  const int smem = r.tiles_per_split * (2 * 64 * D * 2 + 64 * 4 + 8);
+  static const hipError_t set = [] {
+    constexpr int most = kHeldBytes + kHeldBytes / (2 * 64 * D * 2) * (64 * 4 + 8);
+    hipError_t e = hipFuncSetAttribute((const void*)held_attn<D, NW, false, false>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)held_attn<D, NW, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)held_attn<D, NW, false, true>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e;
+  }();
+  if (set != hipSuccess) return DF_EHIP;
+  const dim3 grid((unsigned)((long long)r.row_groups * r.nsplit * p.kv_heads * p.B)), wg(64 * NW);
+  if (cached) hipLaunchKernelGGL((held_attn<D, NW, false, true>), grid, wg, smem, st, p, r.row_groups, r.own_tiles);
+  else if (masked) hipLaunchKernelGGL((held_attn<D, NW, true, false>), grid, wg, smem, st, p, r.row_groups, r.own_tiles);
+  else hipLaunchKernelGGL((held_attn<D, NW, false, false>), grid, wg, smem, st, p, r.row_groups, r.own_tiles);
+  return DF_OK;
 }
 
 int launch_qattn(const QAttnArgs& a, hipStream_t st) {
   const bool cached = a.cache != nullptr;
   const long long rows = (long long)a.Lq * (a.heads / a.kv_heads), own = a.own_period > 0 ? (long long)a.own_n * (a.L / a.own_period) : a.own_n;
   const long long keys0 = cached ? a.L - own : a.L;
-  const Plan r = plan_of(a.B, rows, a.kv_heads, a.d, keys0, own, cached, a.mask != nullptr, a.dtype);
-  if (rows > 0x7fffffffLL - 256 || (long long)a.B * a.kv_heads * rows * (a.d / 8) >= (1LL << 32) - 256) return DF_ESHAPE;
+  const Plan r = plan_of(Task{a.B, a.kv_heads, a.d, a.dtype, rows, a.L, own, a.own_lo, cached, a.mask != nullptr, a.own_period > 0});
+  if (!r.ok || rows > 0x7fffffffLL - 256 || (long long)a.B * a.kv_heads * rows * (a.d / 8) >= (1LL << 32) - 256) return DF_ESHAPE;
   if (a.workspace_bytes < r.expand + r.parts || (r.expand + r.parts && !a.workspace)) return DF_ENOMEM;
   QParams p = {};
   p.q = a.q; p.ldq = a.ldq; p.bsq = a.bsq; p.out = a.out;
@@ -681,7 +1429,7 @@ int launch_qattn(const QAttnArgs& a, hipStream_t st) {
   p.nsplit = r.nsplit; p.tiles_per_split = r.tiles_per_split;
   p.mask = a.mask; p.lens = a.lens;
   p.part_o = (float*)((char*)a.workspace + r.expand);
-  p.part_ml = p.part_o + (size_t)r.nsplit * a.B * a.kv_heads * rows * a.d;
+  p.part_ml = p.part_o + (r.kind == kRows ? (size_t)r.share.count * 2 * r.block : (size_t)r.nsplit * a.B * a.kv_heads * rows) * a.d;
   if (cached) {
     p.c = kv4_view(a.cache, a.B, a.L, a.kv_heads, a.d);
     p.own_lo = a.own_lo; p.own_n = a.own_n; p.own_period = a.own_period;
@@ -693,7 +1441,7 @@ int launch_qattn(const QAttnArgs& a, hipStream_t st) {
   rows_seg.k = a.k; rows_seg.v = a.v; rows_seg.ldk = a.ldk; rows_seg.ldv = a.ldv; rows_seg.bsk = a.bsk; rows_seg.bsv = a.bsv;
   rows_seg.hsk = rows_seg.hsv = a.d;
   if (cached) rows_seg.n = (int)own;
-  const long long nwg = (rows + r.block - 1) / r.block * a.kv_heads * a.B * r.nsplit;
+  const long long nwg = r.kind == kRows ? r.share.count : r.kind == kHeld ? (long long)r.row_groups * a.kv_heads * a.B * r.nsplit : (rows + r.block - 1) / r.block * a.kv_heads * a.B * r.nsplit;
   if (nwg > 0x7fffffffLL) return DF_ESHAPE;
   const dim3 grid((unsigned)nwg);
   if (r.expand) {
@@ -722,8 +1470,15 @@ int launch_qattn(const QAttnArgs& a, hipStream_t st) {
     else if (a.d == 64) hipLaunchKernelGGL((few_rows_kv4<64, 2>), grid, dim3(256), 0, st, p);
     else if (r.nq == 1) hipLaunchKernelGGL((few_rows_kv4<128, 1>), grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL((few_rows_kv4<128, 2>), grid, dim3(256), 0, st, p);
+  } else if (r.kind == kHeld) {
+    const bool masked = a.mask != nullptr;
+    const int rc = a.d <= 64 ? (r.nq == 8 ? launch_held<64, 8>(p, r, masked, cached, st) : launch_held<64, 4>(p, r, masked, cached, st))
+                             : (r.nq == 8 ? launch_held<128, 8>(p, r, masked, cached, st) : launch_held<128, 4>(p, r, masked, cached, st));
+    if (rc != DF_OK) return rc;
   } else {
-    const int rc = a.d <= 64 ? launch_rows<64, 4>(p, a.mask != nullptr, grid, st) : launch_rows<128, 8>(p, a.mask != nullptr, grid, st);
+    const bool masked = a.mask != nullptr;
+    const int rc = a.d <= 64 ? (r.nq == 1 ? launch_rows<64, 1>(p, r, masked, st) : launch_rows<64, 2>(p, r, masked, st))
+                             : launch_rows<128, 1>(p, r, masked, st);
     if (rc != DF_OK) return rc;
   }
   DF_LAUNCH_CHECK();

@@ -109,5 +109,5 @@ def test_workspace_of_sizes_that_are_not_taken():
     L = df.lib()
     assert L.df_cross_attn_workspace_bytes(1, 1, 64, 1, 1, 200, 0, 1) == 0
     assert L.df_attn_kv4_workspace_bytes(1, 1, 64, 1, 1, 96, 1) == 0
-    assert L.df_attn_displaced_kv4_workspace_bytes(1, 8, 8, 1, 1, 64, 5, 1) == 0
+    assert L.df_attn_displaced_kv4_workspace_bytes(1, 8, 8, 1, 1, 64, 0, 5, 1, 0) == 0
     assert L.df_attn_kv4_workspace_bytes(1, 1, 57600, 1, 1, 64, 1) > 0

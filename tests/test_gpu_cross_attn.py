@@ -73,6 +73,39 @@ def test_scores_far_apart_and_without_a_number(bf16):
     assert df.cross_attn(q.abs(), w, v, lens=lens).isnan().all()                       # every score -inf: the formula has no value
 
 
+@pytest.mark.parametrize("Lq,Lk,heads,kv,d", [(130, 60, 600, 600, 64), (130, 130, 600, 600, 64), (70, 300, 600, 600, 64), (130, 1000, 600, 600, 64),
+                                              (130, 1000, 700, 350, 64), (70, 200, 600, 600, 128), (20, 900, 600, 300, 72)])
+def test_more_blocks_of_rows_than_workgroups(Lq, Lk, heads, kv, d):
+    """Workgroups that go from block to block, and blocks that are cut between two of them."""
+    print("blocks", Lq, Lk, heads, kv, d, flush=True)
+    q, k, v = _rows(1, 1, Lq, heads, d), _rows(2, 1, Lk, kv, d), _rows(3, 1, Lk, kv, d)
+    mask = torch.rand(1, Lk, generator=torch.Generator().manual_seed(5)) < 0.7
+    mask[0, 64:128] = False
+    out = df.cross_attn(q, k, v), df.cross_attn(q, k, v, key_mask=mask.to(DEV)), df.cross_attn(q, k, v, lens=torch.tensor([Lk - 7], dtype=torch.int32, device=DEV))
+    valid = None, mask.numpy(), np.arange(Lk)[None] < Lk - 7
+    g = heads // kv
+    for h in (0, 1, kv // 2, kv - 2, kv - 1):                # some heads: the others are the same kernel's
+        for got, ok in zip(out, valid):
+            _check(got[:, :, h * g:(h + 1) * g], q[:, :, h * g:(h + 1) * g], host(k[:, :, h:h + 1]), host(v[:, :, h:h + 1]), True, ok)
+    from_f32 = df.cross_attn(q[:, :, :g].float(), k[:, :, :1].float(), v[:, :, :1].float())
+    assert torch.allclose(out[0][:, :, :g].float(), from_f32, rtol=0.05, atol=0.05)
+    one = [torch.cat([df.cross_attn(q[:, :, h * g:(h + 1) * g].contiguous(), k[:, :, h:h + 1].contiguous(), v[:, :, h:h + 1].contiguous())]) for h in range(0, kv, 37)]
+    for i, h in enumerate(range(0, kv, 37)):
+        assert torch.allclose(out[0][:, :, h * g:(h + 1) * g].float(), one[i].float(), rtol=0.02, atol=0.02)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("Lq,Lk,heads", [(5, 3000, 1), (300, 5000, 2), (40, 130, 1)])
+def test_parts_whose_scores_are_all_minus_infinity(Lq, Lk, heads, bf16):
+    """Keys are split over workgroups: one that sees none but scores of -inf has no share in the others' result."""
+    q, k, v = _rows(1, 1, Lq, heads, 64, bf16=bf16).abs(), _rows(2, 1, Lk, heads, 64, bf16=bf16), _rows(3, 1, Lk, heads, 64, bf16=bf16)
+    w = k.clone()
+    w[:, :Lk // 2] = float("-inf")
+    valid = np.broadcast_to(np.arange(Lk)[None] >= Lk // 2, (1, Lk))
+    _check(df.cross_attn(q, w, v), q, host(k), host(v), bf16, valid)
+    assert df.cross_attn(q, torch.full_like(k, float("-inf")), v).isnan().all()
+
+
 def test_the_same_bits_and_a_given_result():
     q, k, v = _rows(1, 2, 50, 4, 64), _rows(2, 2, 900, 2, 64), _rows(3, 2, 900, 2, 64)
     out = torch.empty_like(q)
