@@ -385,6 +385,8 @@ static inline int qattn_sizes(int B, int Lq, long long L, int heads, int kv_head
   if (d <= 0 || d % 8 || d > 128 || heads > (1 << 20) || (long long)Lq * (heads / kv_heads) > 0x7fffffffLL - 256) return DF_ESHAPE;
   return (long long)B * Lq * heads * (d / 8) < (1LL << 32) - 256 ? DF_OK : DF_ESHAPE;
 }
+// Rows of keys and values: the kernels' offsets within a tile of them are 32 bits
+static inline bool far_rows(long long rows, long long k_ld, long long v_ld) { return rows > 1 && (k_ld > (1LL << 24) || v_ld > (1LL << 24)); }
 static inline bool bad_workspace(const void* w) { return (uintptr_t)w % 256 != 0; }
 
 size_t df_cross_attn_workspace_bytes(int B, int Lq, int Lk, int heads, int kv_heads, int d, int masked, int dtype) {
@@ -400,6 +402,7 @@ int df_cross_attn(const void* q, long long q_ld, long long q_bs, const void* k, 
   if ((uintptr_t)out % 16 || (uintptr_t)lens % 4 || bad_workspace(workspace)) return DF_EINVAL;
   const int rc = qattn_sizes(B, Lq, Lk, heads, kv_heads, d);
   if (rc != DF_OK) return rc;
+  if (far_rows(Lk, k_ld, v_ld)) return DF_ESHAPE;
   QAttnArgs a = {};
   a.q = q; a.k = k; a.v = v; a.out = out; a.mask = key_mask; a.lens = lens;
   a.ldq = q_ld; a.bsq = q_bs; a.ldk = k_ld; a.bsk = k_bs; a.ldv = v_ld; a.bsv = v_bs;
@@ -448,6 +451,7 @@ int df_attn_displaced_kv4(const void* q, long long q_ld, long long q_bs, const v
   a.L = H * W; a.Lq = a.L / N;
   rc = qattn_sizes(B, a.Lq, a.L, heads, kv_heads, d);
   if (rc != DF_OK) return rc;
+  if (far_rows(a.Lq, k_ld, v_ld)) return DF_ESHAPE;
   a.q = q; a.k = k_fresh; a.v = v_fresh; a.cache = cache; a.out = out;
   a.ldq = q_ld; a.bsq = q_bs; a.ldk = k_ld; a.bsk = k_bs; a.ldv = v_ld; a.bsv = v_bs;
   a.B = B; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.dtype = dtype; a.scale = scale;

@@ -69,9 +69,6 @@ __device__ __forceinline__ void place(const QParams& p, int nrb, int& rb, int& k
   b = t / p.kv_heads;
 }
 
-// Tiles of 64 keys that a workgroup sums over: those of segment 0 that have a key, then segment 1's
-constexpr int kListTiles = 1024;               // tiles of one split whose words are kept (masks)
-
 // ---- bf16 rows ----
 // A workgroup is four waves of QB * 32 rows.  The work is a line of tiles of 64 keys, block of rows by block of rows; workgroup w takes the w-th of
 // equal shares of it (`Share`), so all end together whatever the number of blocks: a share that covers a block writes its result, one that
@@ -88,6 +85,23 @@ __host__ __device__ inline unsigned int share_of(const Share& s, unsigned int ti
   return tile < big ? tile / (s.per + 1) : s.more + (tile - big) / s.per;
 }
 
+// Where lengths (or the number of rows that a mask leaves) are known on the device only, the shares are those of the longest batch item: as many as
+// planned, of the keys there are.
+__device__ __forceinline__ Share share_of_keys(const QParams& p, Share s, int nrb) {
+  if (!p.lens) return s;
+  int longest = 0;
+  for (int b = threadIdx.x & 63; b < p.B; b += 64) longest = max(longest, seg0_rows(p, b));
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, 64));
+  longest = __builtin_amdgcn_readfirstlane(longest);
+  const unsigned int tiles = (unsigned int)(((longest + 63) >> 6) + ((p.seg[1].n + 63) >> 6)), planned = s.tiles;
+  s.tiles = tiles > 0 ? tiles : 1;
+  s.all = s.tiles * (unsigned int)(nrb * p.kv_heads * p.B);
+  if (s.more == 0 && s.per % planned == 0) s.per = s.per / planned * s.tiles;      // whole blocks
+  else { s.per = s.all / s.count; s.more = s.all % s.count; }
+  return s;
+}
+
 // The loop is software-pipelined inside the wave, since matrix instructions and the softmax's vector instructions of a SIMD overlap only where one
 // wave's stream mixes them: iteration t issues S_{t+1} = K_{t+1} Q^T and O += V_{t-1} P_{t-1} between the exponentials of tile t, whose registers
 // take S_{t+1} as they come free.  K and V tiles go memory -> LDS by direct loads, K_{t+3} and V_{t+1} in iteration t, to rings of four slots (so
@@ -96,13 +110,14 @@ __host__ __device__ inline unsigned int share_of(const Share& s, unsigned int ti
 // The running maximum is that of the first tile and moves when a row's weights of a tile sum to more than 2^13 (the sums are needed anyway; the
 // maximum of every tile would be 22 instructions more): by the power of two above the sum, which scales the packed weights exactly, or, beyond 2^100,
 // to the tile's own maximum, with the tile done again from its K in LDS.
-template <int D, int QB, bool MASK>
-__global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QParams p, Share sh) {
+template <int D, int QB>
+__global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QParams p, Share planned) {
   constexpr int TILE = 64 * D * 2, CH = D / 8, KS = D / 16, DB = D / 32, LPT = TILE / 4096, RPI = 1024 / (D * 2), M = D / 64, BLK = 128 * QB;
-  extern __shared__ __attribute__((aligned(16))) char smem[];             // four K tiles, four V tiles; MASK: words and tiles
+  extern __shared__ __attribute__((aligned(16))) char smem[];             // four K tiles, four V tiles
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, c = lane & 31, csig = (c & 0x13) | ((c & 4) << 1) | ((c & 8) >> 1), tri = lane & 15;
   const int nrb = (p.rows + BLK - 1) / BLK;
+  const Share sh = share_of_keys(p, planned, nrb);
   unsigned int w;
   {
     const unsigned int t = blockIdx.x, xcd = t & 7, base = sh.count >> 3, rem = sh.count & 7;   // an XCD takes shares side by side: the same keys
@@ -110,8 +125,6 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
   }
   unsigned int pos = share_begin(sh, w);
   const unsigned int end = share_begin(sh, w + 1);
-  unsigned long long* words = (unsigned long long*)(smem + 8 * TILE);     // MASK: of the tiles that have a key
-  unsigned short* list = (unsigned short*)(words + kListTiles);
   // Direct load j of the wave covers tile rows (LPT wave + j) * RPI + lane / CH; the chunks of a row are swizzled by it.  Values beyond d are read as
   // the first ones (Q is 0 there, those of O are dropped).
   unsigned int kch[LPT], vch[LPT];
@@ -189,41 +202,14 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
   Block blk = open(), after = blk;
   bool primed = false;                                     // the last block's final iterations have requested this one's first tiles and Q
   int s0 = 0;                                              // slot of its tile 0
-  int listed = 0;                                          // MASK: tiles of the list
-  for (bool more = true, same = false; more;) {
+  for (bool more = true; more;) {
     more = pos < end;
     if (more) after = open();
     if (!primed) queries(blk);
-    if constexpr (MASK) {
-      if (!same) {
-        __syncthreads();                                   // (the last block's list has been read)
-        for (int i = wave; i < blk.nt; i += 4) {
-          const int key = (blk.lo + i) * 64 + lane;
-          const unsigned long long bits = __builtin_amdgcn_ballot_w64(key < blk.n0 && p.mask[(long long)blk.b * p.seg[0].n + key] != 0);
-          if (lane == 0) words[i] = bits;
-        }
-        __syncthreads();
-        // the tiles with a key move to the front (wave 0; every chunk is read before it is written, in front of itself)
-        if (wave == 0) {
-          int at = 0;
-          for (int i = 0; i < blk.nt; i += 64) {
-            const unsigned long long bits = i + lane < blk.nt ? words[i + lane] : 0ULL;
-            const unsigned long long some = __builtin_amdgcn_ballot_w64(bits != 0);
-            const int to = at + __popcll(some & low_bits(lane));
-            if (bits) { words[to] = bits; list[to] = (unsigned short)(i + lane); }
-            at += __popcll(some);
-          }
-          if (lane == 0) *(int*)(list + kListTiles) = at;
-        }
-        __syncthreads();
-        listed = __builtin_amdgcn_readfirstlane(*(volatile int*)(list + kListTiles));
-      }
-      same = more && after.b == blk.b && after.lo == blk.lo && after.nt == blk.nt;
-    }
-    const int nt = MASK ? listed : blk.nt, ant = MASK ? listed : after.nt;
+    const int nt = blk.nt, ant = after.nt;
     // The next block's first tiles follow this one's last (of which a block that was itself begun ahead has three at least: the slots behind a
     // shorter one hold its last tile again)
-    const bool ahead = more && nt > 0 && ant > 0 && (!MASK || same) && (!primed || nt >= 3);
+    const bool ahead = more && nt > 0 && ant > 0 && (!primed || nt >= 3);
     const int lo = blk.lo, n0 = blk.n0, n1 = p.seg[1].n, tiles0 = blk.tiles0, b = blk.b, kh = blk.kh, row0 = blk.row0;
     const bool whole = blk.whole, idle = row0 >= p.rows;
     const unsigned int slot = 2 * w + (lo == 0 ? 1 : 0);
@@ -235,32 +221,25 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
         asm volatile("" : "+v"(qreg[n][s]));               // Q has arrived: the loop does not wait for it, with the direct loads
       }
 
-    // Tile i of the list and which of its keys count.  Past the end: the next block's, or the last one again, which keeps the counts of loads in
+    // Tile i and which of its keys count.  Past the end: the next block's, or the last one again, which keeps the counts of loads in
     // flight uniform.
     struct Info { int t; bool next; unsigned long long w; };
     auto info = [&](int i) DF_INLINE {
       Info r;
       r.next = i >= nt && ahead;
       if (i >= nt) i = !ahead ? nt - 1 : i - nt < ant ? i - nt : ant - 1;
-      if constexpr (MASK) {
-        const unsigned long long bits = words[i];
-        r.t = lo + __builtin_amdgcn_readfirstlane((int)list[i]);
-        r.w = (unsigned long long)(unsigned int)__builtin_amdgcn_readfirstlane((int)bits) |
-              (unsigned long long)(unsigned int)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32;
-      } else {
-        const int z0 = r.next ? after.tiles0 : tiles0;
-        r.t = (r.next ? after.lo : lo) + i;
-        r.w = r.t < z0 ? low_bits((r.next ? after.n0 : n0) - r.t * 64) : low_bits(n1 - (r.t - z0) * 64);
-      }
+      const int z0 = r.next ? after.tiles0 : tiles0;
+      r.t = (r.next ? after.lo : lo) + i;
+      r.w = r.t < z0 ? low_bits((r.next ? after.n0 : n0) - r.t * 64) : low_bits(n1 - (r.t - z0) * 64);
       return r;
     };
-    // Where the wave's loads of a tile come from.  Keys that are none are read as one that is: their weight is 0, the value must be finite where
-    // the others are.
+    // Where the wave's loads of a tile come from.  Rows behind the last key are read as one that is: their weight is 0, the value must be finite
+    // where the others are.
     struct Source { const char* base; unsigned int ofs[LPT]; };
     auto source = [&](auto isv, const Info& i) DF_INLINE {
       constexpr bool V = decltype(isv)::value;
       const int z0 = i.next ? after.tiles0 : tiles0;
-      const bool second = !MASK && i.t >= z0;
+      const bool second = i.t >= z0;
       const Seg& s = p.seg[second ? 1 : 0];
       const int ld = (int)(V ? s.ldv : s.ldk);
       Source r;
@@ -292,27 +271,8 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
         for (int e = 0; e < 16; ++e) o[n][i][e] = 0.f;
       m[n] = kLow; l[n] = 0.f;
     }
-    // MASK: where the scores start, 0 or, for a key that is none, -infinity: 64 floats per tile, a slot beside its K
-    float* const bias = (float*)((char*)list + kListTiles * 2 + 16);
-    f32x16 start[2];
-    auto fetch_start = [&](int at, int kb) DF_INLINE {
-      if constexpr (MASK) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>((char*)bias + at / TILE * 256 + (32 * kb + 16 * (i >> 1) + 8 * g + 4 * (i & 1)) * 4);
-          start[kb][4 * i] = v.x; start[kb][4 * i + 1] = v.y; start[kb][4 * i + 2] = v.z; start[kb][4 * i + 3] = v.w;
-        }
-      }
-    };
-    auto put_start = [&](int i, unsigned long long bits) DF_INLINE {       // by one wave, two barriers before it is read
-      if (MASK && wave == (i & 3)) bias[((s0 + i) & 3) * 64 + lane] = (bits >> lane) & 1 ? 0.f : -INFINITY;
-    };
     auto s_mfma = [&](u32x4 k, int s, int kb, int n) DF_INLINE {
       if (s == 0) {
-        if constexpr (MASK) {
-          sa[n][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), qreg[n][s], start[kb], 0, 0, 0);
-          return;
-        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) sa[n][kb][e] = 0.f;
       }
@@ -323,8 +283,6 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
     };
     auto scores = [&](int i) DF_INLINE {
       const int kt = slot_of(s0 + i);
-      fetch_start(kt, 0);
-      fetch_start(kt, 1);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -335,7 +293,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
         }
     };
     auto hide = [&](unsigned long long bits) DF_INLINE {             // scores of keys that are none
-      if (MASK || bits == ~0ULL) return;
+      if (bits == ~0ULL) return;
       const unsigned long long mine = bits >> (8 * g);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -429,13 +387,13 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
           case 0: E(0, 0); break;
           case 1: E(0, 1); load(ka, 0, kd); break;
           case 2: C(0); load(ka, 1, kd); break;
-          case 3: E(1, 0); fetch_start(kt, 0); break;
+          case 3: E(1, 0); break;
           case 4: E(1, 1); break;
           case 5: C(1); S(0); break;
           case 6: E(2, 0); if constexpr (LPT > 2) load(ka, 2, kd); break;
           case 7: E(2, 1); S(1); break;
           case 8: C(2); load(va, 0, vd); break;
-          case 9: E(3, 0); fetch_start(kt, 1); break;
+          case 9: E(3, 0); break;
           case 10: E(3, 1); load(va, 1, vd); break;
           case 11: S(2); if constexpr (LPT > 2) load(ka, 3, kd); break;
           case 12: C(3); if constexpr (LPT > 2) load(va, 2, vd); break;
@@ -494,7 +452,6 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
       if (!primed) {
         s0 = 0;
         block_sync();                                      // (every wave's reads of the last block are done: they were waited for)
-        put_start(0, cur.w); put_start(1, n1i.w); put_start(2, n2i.w);
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
           ka = source(IsK{}, i == 0 ? cur : i == 1 ? n1i : n2i);
@@ -507,11 +464,10 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
         sync_tile();
       }
       auto next = [&](int t) DF_INLINE { cur = n1i; n1i = n2i; n2i = n3i; n3i = info(t + 4); };
-      // an iteration's loads, the starts of the scores of tile t + 3, and at the last one the next block's Q
+      // an iteration's loads, and at the last one the next block's Q
       auto begin = [&](int t) DF_INLINE {
         ka = source(IsK{}, n3i);
         va = source(IsV{}, n1i);
-        put_start(t + 3, n3i.w);
         if (t == nt - 1 && ahead) queries(after);
       };
       if (idle) {
@@ -548,9 +504,9 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
         sync_tile();
         int t = 1;
         while (t < nt) {
-          if constexpr (!MASK) {
-            // tiles t .. t + 3 whole and of one segment: as long as that holds
-            const int at = lo + t, second = at >= tiles0;
+          // Tiles t .. t + 3 whole and of one segment: as long as that holds.  (Without a scope of their own its values spill, 400 bytes of them.)
+          {
+            const int second = lo + t >= tiles0;
             int run = (second ? tiles0 + (n1 >> 6) : n0 >> 6) - lo;
             if (run > nt) run = nt;
             if (t + 3 < run) {
@@ -663,8 +619,9 @@ __device__ __forceinline__ void merge_parts(const QParams& p, int n, int at, F w
 
 // The parts of a block that shares cut: its first share's (slot 2 w + 1), then those of the shares that begin inside it (slot 2 w), in that order.
 // Eight values of a row per lane.
-__global__ __launch_bounds__(256) void merge_shares(QParams p, Share sh, int blk, unsigned int per_row) {
+__global__ __launch_bounds__(256) void merge_shares(QParams p, Share planned, int blk, unsigned int per_row) {
   const unsigned int nrb = (unsigned int)(p.rows + blk - 1) / blk, block = blockIdx.x;
+  const Share sh = share_of_keys(p, planned, (int)nrb);
   const unsigned int w0 = share_of(sh, block * sh.tiles), w1 = share_of(sh, block * sh.tiles + sh.tiles - 1);
   if (w0 == w1) return;
   const unsigned int idx = blockIdx.y * 256 + threadIdx.x;
@@ -678,6 +635,50 @@ __global__ __launch_bounds__(256) void merge_shares(QParams p, Share sh, int blk
   for (int e = 0; e < 8; ++e) o[e] *= inv;
   const long long ld = (long long)p.kv_heads * p.group * p.d;
   st_vec((bf16_t*)p.out + row_offset(p, b, kh, row, (long long)p.Lq * ld, ld) + at, o);
+}
+
+// Rows of segment 0 that the mask (and the length) leaves, side by side per head, and how many they are per batch item: the pipelined loop then has
+// whole tiles of keys, and none for what is masked (its own words and biases per tile cost it 20 us of 150 at 7200 queries, 5120 keys, 10 heads of
+// 64, with every key there).  A workgroup copies those of 64 rows of a head; it counts the ones before them itself.
+__global__ __launch_bounds__(256) void keep_rows(QParams p, int tiles, bf16_t* ko, bf16_t* vo, int* counts) {
+  __shared__ int before[4];
+  __shared__ unsigned long long word;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tile = (int)(blockIdx.x % tiles), bh = (int)(blockIdx.x / tiles), b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
+  const int n = p.seg[0].n, n0 = seg0_rows(p, b);
+  const unsigned char* mask = p.mask + (long long)b * n;
+  const int row0 = tile * 64, upto = row0 < n0 ? row0 : n0;
+  int mine = 0;
+  for (int i = tid * 16; i + 16 <= upto; i += 4096) {
+    unsigned int x[4];
+    __builtin_memcpy(x, mask + i, 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine += __popc((((x[e] & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x[e]) & 0x80808080u);        // bytes that are not 0
+  }
+  if (tid < (upto & 15)) mine += mask[(upto & ~15) + tid] != 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
+  if (lane == 0) before[wave] = mine;
+  if (wave == 0) {
+    const unsigned long long w = __builtin_amdgcn_ballot_w64(row0 + lane < n0 && mask[row0 + lane] != 0);
+    if (lane == 0) word = w;
+  }
+  __syncthreads();
+  const int first = before[0] + before[1] + before[2] + before[3];
+  const unsigned long long w = word;
+  if (tile == tiles - 1 && kh == 0 && tid == 0) counts[b] = first + __popcll(w);
+  const Seg& s = p.seg[0];
+  const bf16_t* k = (const bf16_t*)s.k + (long long)b * s.bsk + (long long)kh * s.hsk;
+  const bf16_t* v = (const bf16_t*)s.v + (long long)b * s.bsv + (long long)kh * s.hsv;
+  const long long to0 = ((long long)b * p.kv_heads + kh) * n + first;
+  const int chunks = p.d / 8;
+  for (int i = tid; i < 64 * chunks; i += 256) {
+    const int r = i / chunks, at = (i - r * chunks) * 8;
+    if (!((w >> r) & 1)) continue;
+    const long long to = (to0 + __popcll(w & low_bits(r))) * p.d + at;
+    *reinterpret_cast<u32x4*>(ko + to) = *reinterpret_cast<const u32x4*>(k + (row0 + r) * s.ldk + at);
+    *reinterpret_cast<u32x4*>(vo + to) = *reinterpret_cast<const u32x4*>(v + (row0 + r) * s.ldv + at);
+  }
 }
 
 // ---- few keys ----
@@ -1233,7 +1234,7 @@ struct Plan {
   int row_groups, own_tiles;                   // kHeld
   Share share;                                 // kRows
   bool ok;
-  size_t expand, parts;                        // bytes of the workspace: the cache's rows in bf16, the parts of the splits or shares
+  size_t expand, parts;                        // bytes of the workspace: the cache's, or a mask's, rows in bf16, the parts of the splits or shares
 };
 
 // What an attention is to be planned for: `own` of `L` keys are fresh rows beside a cache, in a row from own_lo on (or not: own_period)
@@ -1285,8 +1286,9 @@ double plan_rows(const Task& k, int qb, Plan& r) {
   r.ok = true;
   const long long heads = (long long)k.B * k.kv_heads, keys0 = k.cached ? k.L - k.own : k.L, keys1 = k.cached ? k.own : 0;
   r.kind = kRows; r.nq = qb; r.block = 128 * qb; r.tile = 64;
-  const long long tiles = (keys0 + 63) / 64 + (keys1 + 63) / 64, blocks = heads * ((k.rows + r.block - 1) / r.block), all = blocks * tiles;
-  if (k.cached) r.expand = (size_t)(heads * keys0 * k.d * 4 + 255) / 256 * 256;
+  const long long tiles0 = (keys0 + 63) / 64 + (keys1 + 63) / 64, tiles = tiles0 > 0 ? tiles0 : 1;
+  const long long blocks = heads * ((k.rows + r.block - 1) / r.block), all = blocks * tiles;
+  if (k.cached || k.masked) r.expand = ((size_t)heads * keys0 * k.d * 4 + 255) / 256 * 256 + (k.masked ? ((size_t)k.B * 4 + 255) / 256 * 256 : 0);
   // Whole blocks, the same number each, where that takes hardly longer than cutting the line into as many equal shares as workgroups fit the chip
   // (the parts and their merge cost about as much as kCut tiles); shares of four tiles or more.
   constexpr long long kCut = 10;
@@ -1295,12 +1297,11 @@ double plan_rows(const Task& k, int qb, Plan& r) {
   if (!r.ok) return 1e30;
   Share& s = r.share;
   s.tiles = (unsigned int)tiles; s.all = (unsigned int)all;
-  if (rounds * tiles <= (all + fit - 1) / fit + kCut && (!k.masked || tiles <= kListTiles)) {
+  if (rounds * tiles <= (all + fit - 1) / fit + kCut) {
     s.per = (unsigned int)(rounds * tiles);
     s.count = (unsigned int)((blocks + rounds - 1) / rounds);
   } else {
     long long n = all / 4 < fit ? all / 4 : fit;
-    if (k.masked && n < all / (kListTiles - 1) + 1) n = all / (kListTiles - 1) + 1;
     if (n < 1) n = 1;
     s.count = (unsigned int)n; s.per = (unsigned int)(all / n); s.more = (unsigned int)(all % n);
     r.parts = (size_t)n * 2 * r.block * (k.d + 2) * sizeof(float);
@@ -1308,7 +1309,7 @@ double plan_rows(const Task& k, int qb, Plan& r) {
   const bool two = fit == 512 && s.count > 256;
   const double tile = k.d > 64 ? 1.1 : qb == 2 ? 1.05 : two ? 1.16 : 0.85;
   return (k.d > 64 || qb == 2 ? 7.7 : 6.2) + tile * (double)(s.per + 1) * (double)((s.count + fit - 1) / fit) +
-         (r.parts ? merge_us(1.2 * (double)s.count * r.block, k.d) : 0.0) + (k.cached ? 4.0 + (double)(heads * keys0) * k.d * 4.5 / 4e6 : 0.0);
+         (r.parts ? merge_us(1.2 * (double)s.count * r.block, k.d) : 0.0) + (k.cached || k.masked ? 4.0 + (double)(heads * keys0) * k.d * (k.cached ? 4.5 : 8.0) / 4e6 : 0.0);
 }
 
 Plan choose(const Task& k) {
@@ -1371,15 +1372,11 @@ const Plan& plan_of(const Task& k) {
 }
 
 template <int D, int QB>
-int launch_rows(const QParams& p, const Plan& r, bool masked, hipStream_t st) {
-  constexpr int smem = 8 * 64 * D * 2, list = kListTiles * 10 + 16 + 4 * 256;
-  static const hipError_t set = [] {
-    const hipError_t e = hipFuncSetAttribute((const void*)rows_attn<D, QB, true>, hipFuncAttributeMaxDynamicSharedMemorySize, smem + list);
-    return e != hipSuccess ? e : hipFuncSetAttribute((const void*)rows_attn<D, QB, false>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-  }();
+int launch_rows(const QParams& p, const Plan& r, hipStream_t st) {
+  constexpr int smem = 8 * 64 * D * 2;
+  static const hipError_t set = hipFuncSetAttribute((const void*)rows_attn<D, QB>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (set != hipSuccess) return DF_EHIP;
-  if (masked) hipLaunchKernelGGL((rows_attn<D, QB, true>), dim3(r.share.count), dim3(256), smem + list, st, p, r.share);
-  else hipLaunchKernelGGL((rows_attn<D, QB, false>), dim3(r.share.count), dim3(256), smem, st, p, r.share);
+  hipLaunchKernelGGL((rows_attn<D, QB>), dim3(r.share.count), dim3(256), smem, st, p, r.share);
   if (r.parts) {
     DF_LAUNCH_CHECK();
     const unsigned int per_row = (unsigned int)(p.d / 8), blocks = (unsigned int)((p.rows + r.block - 1) / r.block * (long long)p.kv_heads * p.B);
@@ -1444,7 +1441,17 @@ int launch_qattn(const QAttnArgs& a, hipStream_t st) {
   const long long nwg = r.kind == kRows ? r.share.count : r.kind == kHeld ? (long long)r.row_groups * a.kv_heads * a.B * r.nsplit : (rows + r.block - 1) / r.block * a.kv_heads * a.B * r.nsplit;
   if (nwg > 0x7fffffffLL) return DF_ESHAPE;
   const dim3 grid((unsigned)nwg);
-  if (r.expand) {
+  if (r.expand && !cached && keys0 > 0) {                  // the rows that the mask leaves, and their number
+    bf16_t *k = (bf16_t*)a.workspace, *v = k + (size_t)a.B * a.kv_heads * keys0 * a.d;
+    int* const counts = (int*)((char*)a.workspace + ((size_t)a.B * a.kv_heads * keys0 * a.d * 4 + 255) / 256 * 256);
+    const int tiles = (int)((keys0 + 63) / 64);
+    hipLaunchKernelGGL(keep_rows, dim3((unsigned)((long long)tiles * a.kv_heads * a.B)), dim3(256), 0, st, p, tiles, k, v, counts);
+    DF_LAUNCH_CHECK();
+    Seg& s = p.seg[0];
+    s.k = k; s.v = v; s.ldk = s.ldv = a.d; s.hsk = s.hsv = keys0 * a.d; s.bsk = s.bsv = keys0 * a.d * a.kv_heads;
+    p.lens = counts;
+  }
+  if (r.expand && cached) {
     Kv4Args e = {};
     e.cache = const_cast<void*>(a.cache); e.B = a.B; e.L = a.L; e.kv_heads = a.kv_heads; e.d = a.d; e.dtype = DF_BF16;
     e.own_lo = a.own_lo; e.own_n = a.own_n; e.own_period = a.own_period;
@@ -1476,9 +1483,7 @@ int launch_qattn(const QAttnArgs& a, hipStream_t st) {
                              : (r.nq == 8 ? launch_held<128, 8>(p, r, masked, cached, st) : launch_held<128, 4>(p, r, masked, cached, st));
     if (rc != DF_OK) return rc;
   } else {
-    const bool masked = a.mask != nullptr;
-    const int rc = a.d <= 64 ? (r.nq == 1 ? launch_rows<64, 1>(p, r, masked, st) : launch_rows<64, 2>(p, r, masked, st))
-                             : launch_rows<128, 1>(p, r, masked, st);
+    const int rc = a.d <= 64 ? (r.nq == 1 ? launch_rows<64, 1>(p, r, st) : launch_rows<64, 2>(p, r, st)) : launch_rows<128, 1>(p, r, st);
     if (rc != DF_OK) return rc;
   }
   DF_LAUNCH_CHECK();

@@ -78,8 +78,8 @@ def _cached(q=A, c=A, lens=None, out=A, B=2, Lq=8, Lk=4096, heads=4, kv=4, d=64,
     return df.lib().df_attn_kv4(q, 256, 1 << 24, c, lens, out, B, Lq, Lk, heads, kv, d, scale, dt, w, wb, None)
 
 
-def _displaced(q=A, k=A, c=A, out=A, B=2, H=8, W=512, heads=4, kv=4, d=64, patch=1, N=2, scale=0.1, dt=df.DF_BF16, axis=0, w=A, wb=1 << 40):
-    return df.lib().df_attn_displaced_kv4(q, 256, 1 << 24, k, 256, 1 << 24, k, 256, 1 << 24, c, out, B, H, W, heads, kv, d, patch, N, scale, dt, axis, w, wb,
+def _displaced(q=A, k=A, c=A, out=A, ld=256, B=2, H=8, W=512, heads=4, kv=4, d=64, patch=1, N=2, scale=0.1, dt=df.DF_BF16, axis=0, w=A, wb=1 << 40):
+    return df.lib().df_attn_displaced_kv4(q, 256, 1 << 24, k, ld, 1 << 24, k, ld, 1 << 24, c, out, B, H, W, heads, kv, d, patch, N, scale, dt, axis, w, wb,
                                           None)
 
 
@@ -99,6 +99,7 @@ def test_attention(call, kw, rc):
     (lambda: _cross(Lq=0), ESHAPE), (lambda: _cross(Lk=0), ESHAPE), (lambda: _cross(Lq=1 << 30, heads=1 << 10), ESHAPE), (lambda: _cached(c=None), EINVAL),
     (lambda: _cached(c=A + 4), EINVAL), (lambda: _cached(lens=A + 2), EINVAL), (lambda: _cached(d=96), ESHAPE), (lambda: _cached(Lk=0), ESHAPE),
     (lambda: _displaced(k=None), EINVAL), (lambda: _displaced(c=None), EINVAL), (lambda: _displaced(axis=2), EINVAL), (lambda: _displaced(patch=2), ESHAPE),
+    (lambda: _cross(ld=(1 << 24) + 8), ESHAPE), (lambda: _displaced(ld=(1 << 24) + 8), ESHAPE),
     (lambda: _displaced(N=3), ESHAPE), (lambda: _displaced(axis=1, N=3), ESHAPE), (lambda: _displaced(d=32), ESHAPE),
 ])
 def test_attention_each(got, rc):

@@ -111,3 +111,25 @@ def test_the_same_bits_and_a_given_result():
     out = torch.empty_like(q)
     assert df.cross_attn(q, k, v, out=out) is out
     assert all(torch.equal(out, df.cross_attn(q, k, v)) for _ in range(3))
+
+
+@pytest.mark.parametrize("masked,lengths", [(True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("Lq,Lk,heads,kv,d", [(2000, 1300, 8, 4, 64), (1500, 900, 8, 8, 128), (1111, 1027, 5, 5, 72), (6000, 4099, 4, 4, 64)])
+def test_batch_items_with_different_numbers_of_keys(Lq, Lk, heads, kv, d, masked, lengths):
+    """Long enough for the pipelined form: the work is shared by the keys there are; what is no key holds NaN."""
+    print("numbers", Lq, Lk, heads, kv, d, masked, lengths, flush=True)
+    B = 4
+    q, fused = _rows(1, B, Lq, heads, d), _rows(2, B, Lk, 2 * kv * d)
+    n = np.array([Lk, 517, 0, 65]) if lengths else np.full(B, Lk)
+    valid = np.arange(Lk)[None] < n[:, None]
+    mask = torch.rand(B, Lk, generator=torch.Generator().manual_seed(6)) < torch.tensor([0.9, 0.5, 1.0, 0.01])[:, None]
+    if masked:
+        mask[1, :200] = False
+        valid = valid & mask.numpy()
+    gone = torch.from_numpy(~valid).to(DEV)
+    fused = torch.where(gone[..., None], torch.full_like(fused, float("nan")), fused)
+    k, v = fused[..., :kv * d].unflatten(-1, (kv, d)), fused[..., kv * d:].unflatten(-1, (kv, d))
+    rows = torch.tensor([0, 1, 127, 128, Lq // 2, Lq - 1])
+    out = df.cross_attn(q, k, v, key_mask=mask.to(DEV) if masked else None, lens=torch.tensor(n, dtype=torch.int32, device=DEV) if lengths else None)
+    assert out.isfinite().all()
+    _check(out[:, rows], q[:, rows], host(k), host(v), True, valid)
