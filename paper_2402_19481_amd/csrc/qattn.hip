@@ -918,19 +918,23 @@ __global__ __launch_bounds__(256) void merge_splits(QParams p, unsigned int per_
 }
 
 // ---- float ----
-// Four waves of 32 rows each share a tile of 32 keys in LDS.  KV4: segment 0 is the cache (own rows masked out), segment 1 rows of floats.
+// A wave takes 32 rows and every kw-th tile of 32 keys, the workgroup's four 128 / kw rows; the kw sums of a row are joined in LDS at the end.  There
+// are no barriers: lane c's operands are rows of K and values of V as they lie in memory, so they go to registers, V of a tile while its scores are
+// summed and K of the next one during O += V P (2048 cycles of matrix instructions per tile at 32 values; waves with the same keys find them in
+// L1).  KV4: segment 0 is the cache (own rows masked out), segment 1 rows of floats.  1200 queries, 333 keys, 8 heads of 32: 14.2 us, where a tile
+// staged in LDS between barriers took 19.2.
 template <int D, bool KV4>
-__global__ __launch_bounds__(256) void float_attn(QParams p) {
-  constexpr int PK = D + 4, PV = D + 8, DB = D / 32, PER = D / 8;
-  __shared__ __attribute__((aligned(16))) float kt[32 * PK], vt[32 * PV];
-  __shared__ float bias[32];
+__global__ __launch_bounds__(256) void float_attn(QParams p, int kw) {
+  constexpr int DB = D / 32;
+  __shared__ float red[3][16 * DB + 2][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
+  const int kg = wave & (kw - 1), group = wave / kw, block = 128 / kw;
   int rb, kh, b, split;
-  place(p, (p.rows + 127) / 128, rb, kh, b, split);
+  place(p, (p.rows + block - 1) / block, rb, kh, b, split);
   const int n0 = seg0_rows(p, b), n1 = p.seg[1].n, tiles0 = (n0 + 31) >> 5, all = tiles0 + ((n1 + 31) >> 5);
   const int lo = split * p.tiles_per_split, hi = lo + p.tiles_per_split < all ? lo + p.tiles_per_split : all;
-  const int row = rb * 128 + wave * 32 + c;
-  const bool have = row < p.rows, idle = rb * 128 + wave * 32 >= p.rows;
+  const int row = rb * block + group * 32 + c;
+  const bool have = row < p.rows;
   float q[D / 2];                                          // values 8 j + 4 g + i at 4 j + i
   {
     const float* qp = (const float*)p.q + row_offset(p, b, kh, have ? row : 0, p.bsq, p.ldq);
@@ -941,110 +945,196 @@ __global__ __launch_bounds__(256) void float_attn(QParams p) {
       q[4 * j] = t.x; q[4 * j + 1] = t.y; q[4 * j + 2] = t.z; q[4 * j + 3] = t.w;
     }
   }
-  f32x16 o[DB];
+  f32x16 o[DB], sa;
 #pragma unroll
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = kLow, l = 0.f;
   bool any = false;                                        // a key so far
-  for (int t = lo; t < hi; ++t) {
-    const bool second = t >= tiles0;
-    const Seg& s = p.seg[second ? 1 : 0];
-    const int key0 = (second ? t - tiles0 : t) * 32, n = second ? n1 : n0;
-    const int r = tid >> 3, part = (tid & 7) * PER, key = key0 + r;
+  auto is_key = [&](int key, int n, bool first) DF_INLINE {
     bool valid = key < n;
-    if (valid && !second && p.mask) valid = p.mask[(long long)b * p.seg[0].n + key] != 0;
-    if (KV4 && valid && !second && p.own_n > 0) {
+    if (valid && first && p.mask) valid = p.mask[(long long)b * p.seg[0].n + key] != 0;
+    if (KV4 && valid && first && p.own_n > 0) {
       const int rel = (p.own_period > 0 ? key % p.own_period : key) - p.own_lo;
       valid = !(rel >= 0 && rel < p.own_n);
     }
-    if (!__syncthreads_or(valid)) continue;                // (also: the last tile's reads are done)
-    any = true;
-    if (!KV4 || second) {
-      const float* k = (const float*)s.k + (long long)b * s.bsk + (long long)kh * s.hsk + (long long)key * s.ldk;
-      const float* v = (const float*)s.v + (long long)b * s.bsv + (long long)kh * s.hsv + (long long)key * s.ldv;
-#pragma unroll
-      for (int i = 0; i < PER; i += 4) {
-        f32x4 a = {0.f, 0.f, 0.f, 0.f}, w = a;
-        if (valid && part + i < p.d) {
-          a = *reinterpret_cast<const f32x4*>(k + part + i);
-          w = *reinterpret_cast<const f32x4*>(v + part + i);
-        }
-        *reinterpret_cast<f32x4*>(kt + r * PK + part + i) = a;
-        *reinterpret_cast<f32x4*>(vt + r * PV + part + i) = w;
-      }
-    } else {
-      const long long head = (long long)b * p.kv_heads + kh, base = head * p.c.pitch;
-      const float sk = valid ? bf2f(p.c.ks[base + key]) : 0.f;
-#pragma unroll
-      for (int i = 0; i < PER; i += 8) {
-        const unsigned int w = *reinterpret_cast<const unsigned int*>(p.c.kc + (base + key) * (D / 2) + (part + i) / 2);
-        const f32x2 a0 = kv4_levels<0>(w), a1 = kv4_levels<1>(w), a2 = kv4_levels<2>(w), a3 = kv4_levels<3>(w);
-        float* to = kt + r * PK + part + i;
-        *reinterpret_cast<f32x4*>(to) = f32x4{a0.x * sk, a0.y * sk, a1.x * sk, a1.y * sk};
-        *reinterpret_cast<f32x4*>(to + 4) = f32x4{a2.x * sk, a2.y * sk, a3.x * sk, a3.y * sk};
-      }
-      for (int idx = tid; idx < D * 4; idx += 256) {       // eight keys of a value
-        const int e = idx >> 2, k8 = (key0 & 32) + 8 * (idx & 3);
-        const unsigned int w = *reinterpret_cast<const unsigned int*>(p.c.vc + (head * (p.c.pitch / 64) + (key0 >> 6)) * (D * 32) + e * 32 + k8 / 2);
-        const f32x2 a[4] = {kv4_levels<0>(w), kv4_levels<1>(w), kv4_levels<2>(w), kv4_levels<3>(w)};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int kk = 8 * (idx & 3) + j;
-          const float x = a[j >> 1][j & 1] * bf2f(p.c.vs[base + key0 + kk]);
-          vt[kk * PV + e] = x;
-        }
-      }
-    }
-    if ((tid & 7) == 0) bias[r] = valid ? 0.f : -INFINITY;
-    __syncthreads();
-    if (idle) continue;
-    f32x16 sa;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sa[e] = 0.f;
-#pragma unroll
-    for (int j = 0; j < D / 8; ++j) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(kt + c * PK + 8 * j + 4 * g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sa = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], q[4 * j + i], sa, 0, 0, 0);
-    }
+    return valid;
+  };
+  // scores of the keys that count -> weights; the keys of element e are 8 (e / 4) + 4 g + e % 4
+  auto weights = [&](unsigned int bits) DF_INLINE {
+    const unsigned int mine = bits >> (4 * g);
     float top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      if (bias[8 * (e >> 2) + 4 * g + (e & 3)] != 0.f) sa[e] = -INFINITY;
+      if (!(mine >> (8 * (e >> 2) + (e & 3)) & 1)) sa[e] = -INFINITY;
       top = fmaxf(top, sa[e]);
     }
     top = fmaxf(top, __shfl_xor(top, 32, 64)) * p.sc;
     const float mn = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mn);
+    if (__builtin_amdgcn_ballot_w64(mn > m)) {
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] *= alpha;
+    }
     m = mn;
-    l *= alpha;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[db][e] *= alpha;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int kk = 8 * (e >> 2) + 4 * g + (e & 3);
-      const float x = __builtin_amdgcn_exp2f(fmaf(sa[e], p.sc, -m));
-      l += x;
+      sa[e] = __builtin_amdgcn_exp2f(fmaf(sa[e], p.sc, -m));
+      l += sa[e];
+    }
+    any = true;
+  };
+  auto scores = [&](const f32x4 (&k)[D / 8]) DF_INLINE {
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        float v = vt[kk * PV + 32 * db + c];
-        if (KV4 && bias[kk] != 0.f) v = 0.f;               // (a row that is none may hold a scale that is none)
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x, o[db], 0, 0, 0);
+    for (int e = 0; e < 16; ++e) sa[e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sa = __builtin_amdgcn_mfma_f32_32x32x2f32(k[j][i], q[4 * j + i], sa, 0, 0, 0);
+  };
+  int t = lo + kg;
+  if constexpr (KV4) {                                     // the cache: codes to registers, levels times scale (exact) before their use
+    const long long head = (long long)b * p.kv_heads + kh, base = head * p.c.pitch;
+    const int end = hi < tiles0 ? hi : tiles0;
+    u32x4 kc[D / 32], vc[DB];
+    u32x2 vs[4];
+    bf16_t ks;
+    bool valid = false;
+    auto load_k = [&](int t) DF_INLINE {
+      valid = is_key(t * 32 + c, n0, true);
+      ks = p.c.ks[base + t * 32 + c];
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) kc[i] = *reinterpret_cast<const u32x4*>(p.c.kc + (base + t * 32 + c) * (D / 2) + 16 * i);
+    };
+    if (t < end) load_k(t);
+    for (; t < end; t += kw) {
+      const unsigned int bits = (unsigned int)__builtin_amdgcn_ballot_w64(valid);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        vc[db] = *reinterpret_cast<const u32x4*>(p.c.vc + (head * (p.c.pitch / 64) + (t >> 1)) * (D * 32) + (32 * db + c) * 32 + (t & 1) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vs[i] = *reinterpret_cast<const u32x2*>(p.c.vs + base + t * 32 + 8 * i + 4 * g);
+      f32x4 k[D / 8];
+      const float sk = valid ? bf2f(ks) : 0.f;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) {
+        const unsigned int w = kc[j >> 2][j & 3] >> (16 * g);
+        const f32x2 x = kv4_levels<0>(w), z = kv4_levels<1>(w);
+        k[j] = f32x4{x.x * sk, x.y * sk, z.x * sk, z.y * sk};
       }
+      if (bits) scores(k);
+      __builtin_amdgcn_sched_barrier(0);
+      if (t + kw < end) load_k(t + kw);
+      if (!bits) continue;
+      weights(bits);
+      const unsigned int mine = bits >> (4 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float sv[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sv[e] = mine >> (8 * i + e) & 1 ? __uint_as_float(e & 1 ? vs[i][e >> 1] & 0xffff0000u : vs[i][e >> 1] << 16) : 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const unsigned int w = vc[db][i] >> (16 * g);
+          const f32x2 x = kv4_levels<0>(w), z = kv4_levels<1>(w);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x * sv[0], sa[4 * i], o[db], 0, 0, 0);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y * sv[1], sa[4 * i + 1], o[db], 0, 0, 0);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(z.x * sv[2], sa[4 * i + 2], o[db], 0, 0, 0);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(z.y * sv[3], sa[4 * i + 3], o[db], 0, 0, 0);
+        }
+      }
+    }
+  }
+  {                                                        // rows of floats; behind the last one it is read again, and what is no key counts as 0
+    constexpr bool first = !KV4;
+    const Seg& s = p.seg[KV4 ? 1 : 0];
+    const int n = KV4 ? n1 : n0, t0 = KV4 ? tiles0 : 0;
+    const float* kp = (const float*)s.k + (long long)b * s.bsk + (long long)kh * s.hsk;
+    const float* vp = (const float*)s.v + (long long)b * s.bsv + (long long)kh * s.hsv;
+    f32x4 k[D / 8];
+    bool valid = false;
+    auto load_k = [&](int t) DF_INLINE {
+      const int key = (t - t0) * 32 + c;
+      valid = is_key(key, n, first);
+      const float* from = kp + (key < n ? key : n - 1) * s.ldk;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) k[j] = *reinterpret_cast<const f32x4*>(from + (8 * j + 4 * g < p.d ? 8 * j + 4 * g : 0));
+    };
+    if (t < hi) load_k(t);
+    for (; t < hi; t += kw) {
+      const unsigned int bits = (unsigned int)__builtin_amdgcn_ballot_w64(valid);
+      float v[DB][16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = (t - t0) * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
+        const float* from = vp + (key < n ? key : n - 1) * s.ldv;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) v[db][e] = from[32 * db + c < p.d ? 32 * db + c : 0];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (bits != 0xffffffffu) {
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j)
+          if (!valid) k[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      scores(k);
+      __builtin_amdgcn_sched_barrier(0);
+      if (t + kw < hi) load_k(t + kw);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!bits) continue;
+      weights(bits);
+      if (bits != 0xffffffffu) {
+        const unsigned int mine = bits >> (4 * g);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            if (!(mine >> (8 * (e >> 2) + (e & 3)) & 1)) v[db][e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db][e], sa[e], o[db], 0, 0, 0);
     }
   }
   l += __shfl_xor(l, 32, 64);
   if (!any) m = -INFINITY;
+  if (kw > 1) {                                            // the sums of a row: the first wave's, then the others in order
+    if (kg) {
+      float(*to)[64] = red[group * (kw - 1) + kg - 1];
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) to[16 * db + e][lane] = o[db][e];
+      to[16 * DB][lane] = m;
+      to[16 * DB + 1][lane] = l;
+    }
+    __syncthreads();
+    if (kg) return;
+    for (int i = 0; i + 1 < kw; ++i) {
+      const float(*from)[64] = red[group * (kw - 1) + i];
+      const float mi = from[16 * DB][lane], mn = fmaxf(m, mi);
+      if (mi == -INFINITY) continue;                       // (no key)
+      const float f = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(mi - mn);
+      l = l * f + from[16 * DB + 1][lane] * w;
+      m = mn;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] = o[db][e] * f + from[16 * db + e][lane] * w;
+    }
+  }
   if (!have) return;
   const long long at0 = ((long long)split * p.B * p.kv_heads + (long long)b * p.kv_heads + kh) * p.rows + row;
   float* to;
   float f = 1.f;
   if (p.nsplit == 1) {
     to = (float*)p.out + row_offset(p, b, kh, row, (long long)p.Lq * p.kv_heads * p.group * p.d, (long long)p.kv_heads * p.group * p.d);
-    f = any ? 1.0f / l : 0.f;
+    f = m != -INFINITY ? 1.0f / l : 0.f;                   // no key: zeros (all scores -inf: 0 / 0, as the formula)
   } else {
     to = p.part_o + at0 * p.d;
     if (g == 0) { p.part_ml[2 * at0] = m; p.part_ml[2 * at0 + 1] = l; }
@@ -1228,7 +1318,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kv4(QParams p) {
 // ---- choice of kernel and splits, all from the arguments' sizes ----
 enum { kRows, kHeld, kFewKv4, kFloat };
 struct Plan {
-  int kind, nq;                                // nq: blocks of 16 (kFewKv4) or of 32 rows a wave (kRows), waves (kHeld)
+  int kind, nq;                                // nq: blocks of 16 (kFewKv4) or of 32 rows a wave (kRows), waves (kHeld), waves on the same rows (kFloat)
   int block, tile;                             // rows of a workgroup, keys of a tile
   int nsplit, tiles_per_split;                 // all but kRows
   int row_groups, own_tiles;                   // kHeld
@@ -1312,17 +1402,49 @@ double plan_rows(const Task& k, int qb, Plan& r) {
          (r.parts ? merge_us(1.2 * (double)s.count * r.block, k.d) : 0.0) + (k.cached || k.masked ? 4.0 + (double)(heads * keys0) * k.d * (k.cached ? 4.5 : 8.0) / 4e6 : 0.0);
 }
 
+// Full precision: `kw` waves of a workgroup on the same rows.  A tile of 32 keys takes a wave 1.55 us at 32 values, 2.6 at 64 and 4.6 at 128 (1200
+// queries, 8 heads of 64 on 2048 keys: kw = 1 with 3 splits 69 us, kw = 2 with one 92, kw = 4 with one 104; 333 keys of 32: 15.1, 14.1, 15.1).
+double plan_float(const Task& k, int kw, long long ns, Plan& r) {
+  r = Plan{};
+  r.ok = true;
+  const long long heads = (long long)k.B * k.kv_heads, own = k.cached ? k.own : 0, tiles = (k.L + 31) / 32 + (own + 31) / 32;
+  r.kind = kFloat; r.nq = kw; r.block = 128 / kw; r.tile = 32;
+  r.tiles_per_split = (int)((tiles + ns - 1) / ns);
+  r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
+  const long long wgs = heads * ((k.rows + r.block - 1) / r.block) * r.nsplit, each = (r.tiles_per_split + kw - 1) / kw;
+  if (wgs > 0x7fffffffLL) return 1e30;
+  if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * k.rows * (k.d + 2) * sizeof(float);
+  const double tile = (0.5 + 1.03 * (k.d <= 32 ? 1 : k.d <= 64 ? 2 : 4)) * (wgs > 256 ? 1.15 : 1.0);
+  return 4.5 + tile * (double)(((wgs + 255) / 256) * each) + (r.nsplit > 1 ? merge_us((double)r.nsplit * heads * k.rows, k.d) : 0.0);
+}
+
 Plan choose(const Task& k) {
   Plan r = {};
   r.ok = true;
   const long long heads = (long long)k.B * k.kv_heads, rows = k.rows, own = k.cached ? k.own : 0;
-  if (k.dtype == DF_F32 || (k.cached && own == 0 && rows <= 64)) {
-    if (k.dtype == DF_F32) { r.kind = kFloat; r.block = 128; r.tile = 32; }
-    else { r.kind = kFewKv4; r.nq = rows > 16 ? 2 : 1; r.block = 16 * r.nq; r.tile = 64; }
-    const long long tiles = (k.L - own + r.tile - 1) / r.tile + (own + r.tile - 1) / r.tile, blocks = heads * ((rows + r.block - 1) / r.block);
+  double best = 1e30;
+  auto offer = [&](double us, const Plan& q) {
+    if (us < best - 1e-9) { best = us; r = q; }
+  };
+  Plan q;
+  if (k.dtype == DF_F32) {
+#ifdef DF_TUNING
+    if (const char* f = tune_env("DF_FLOAT")) {            // waves on the same rows, a colon, splits
+      plan_float(k, f[0] - '0', atoi(f + 2), q);
+      return q;
+    }
+#endif
+    for (int kw = 1; kw <= 4; kw *= 2)
+      for (long long ns = 1; ns <= 32; ++ns)
+        if (ns == 1 || ns * kw * 2 <= (k.L + 31) / 32 + (own + 31) / 32) offer(plan_float(k, kw, ns, q), q);
+    if (best >= 1e29) r.ok = false;
+    return r;
+  }
+  if (k.cached && own == 0 && rows <= 64) {
+    r.kind = kFewKv4; r.nq = rows > 16 ? 2 : 1; r.block = 16 * r.nq; r.tile = 64;
+    const long long tiles = (k.L + 63) / 64, blocks = heads * ((rows + r.block - 1) / r.block);
     long long ns = 1;
-    const long long want = r.kind == kFewKv4 ? 768 : 512;
-    if (blocks < want) ns = want / blocks;
+    if (blocks < 768) ns = 768 / blocks;
     if (ns > tiles / 4) ns = tiles / 4;
     if (ns < 1) ns = 1;
     if (ns > 64) ns = 64;
@@ -1332,11 +1454,6 @@ Plan choose(const Task& k) {
     return r;
   }
   // The form that is predicted to take least
-  double best = 1e30;
-  auto offer = [&](double us, const Plan& q) {
-    if (us < best - 1e-9) { best = us; r = q; }
-  };
-  Plan q;
 #ifdef DF_TUNING
   const char* form = tune_env("DF_QATTN");
   if (form && !strcmp(form, "rows1")) { plan_rows(k, 1, q); return q; }
@@ -1364,7 +1481,7 @@ const Plan& plan_of(const Task& k) {
   thread_local Task last = {};
   thread_local Plan plan = {};
   if (last.B != k.B || last.kv_heads != k.kv_heads || last.d != k.d || last.dtype != k.dtype || last.rows != k.rows || last.L != k.L || last.own != k.own ||
-      last.own_lo != k.own_lo || last.cached != k.cached || last.masked != k.masked || last.period != k.period || tune_env("DF_QATTN")) {
+      last.own_lo != k.own_lo || last.cached != k.cached || last.masked != k.masked || last.period != k.period || tune_env("DF_QATTN") || tune_env("DF_FLOAT")) {
     plan = choose(k);
     last = k;
   }
@@ -1462,16 +1579,11 @@ int launch_qattn(const QAttnArgs& a, hipStream_t st) {
     s.k = k; s.v = v; s.ldk = s.ldv = a.d; s.hsk = s.hsv = keys0 * a.d; s.bsk = s.bsv = keys0 * a.d * a.kv_heads;
   }
   if (r.kind == kFloat) {
-    // (tiles of 32 keys; the cache's own rows stay among segment 0's and are masked)
-    if (cached) {
-      const long long tiles = cdiv(a.L, 32) + cdiv(own, 32);
-      p.tiles_per_split = (int)((tiles + r.nsplit - 1) / r.nsplit);
-    }
-    if (cached && a.d == 64) hipLaunchKernelGGL((float_attn<64, true>), grid, dim3(256), 0, st, p);
-    else if (cached) hipLaunchKernelGGL((float_attn<128, true>), grid, dim3(256), 0, st, p);
-    else if (a.d <= 32) hipLaunchKernelGGL((float_attn<32, false>), grid, dim3(256), 0, st, p);
-    else if (a.d <= 64) hipLaunchKernelGGL((float_attn<64, false>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((float_attn<128, false>), grid, dim3(256), 0, st, p);
+    if (cached && a.d == 64) hipLaunchKernelGGL((float_attn<64, true>), grid, dim3(256), 0, st, p, r.nq);
+    else if (cached) hipLaunchKernelGGL((float_attn<128, true>), grid, dim3(256), 0, st, p, r.nq);
+    else if (a.d <= 32) hipLaunchKernelGGL((float_attn<32, false>), grid, dim3(256), 0, st, p, r.nq);
+    else if (a.d <= 64) hipLaunchKernelGGL((float_attn<64, false>), grid, dim3(256), 0, st, p, r.nq);
+    else hipLaunchKernelGGL((float_attn<128, false>), grid, dim3(256), 0, st, p, r.nq);
   } else if (r.kind == kFewKv4) {
     if (a.d == 64 && r.nq == 1) hipLaunchKernelGGL((few_rows_kv4<64, 1>), grid, dim3(256), 0, st, p);
     else if (a.d == 64) hipLaunchKernelGGL((few_rows_kv4<64, 2>), grid, dim3(256), 0, st, p);
