@@ -54,6 +54,28 @@ __device__ __forceinline__ unsigned int kv4_codes(unsigned int old, float x0, fl
 template <int SEL>
 __device__ __forceinline__ f32x2 kv4_levels(unsigned int w) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, SEL); }
 
+// 8 x 8 nibbles turn: nibble j of a[i] becomes nibble i of a[j] (halves, bytes, nibbles change places: 32 instructions)
+__device__ __forceinline__ void kv4_turn(unsigned int (&a)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned int t = a[i], u = a[i + 4];
+    a[i] = __builtin_amdgcn_perm(u, t, 0x05040100u);
+    a[i + 4] = __builtin_amdgcn_perm(u, t, 0x07060302u);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i += i % 4 == 1 ? 3 : 1) {
+    const unsigned int t = a[i], u = a[i + 2];
+    a[i] = __builtin_amdgcn_perm(u, t, 0x06020400u);
+    a[i + 2] = __builtin_amdgcn_perm(u, t, 0x07030501u);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const unsigned int t = a[i], u = a[i + 1];
+    a[i] = (t & 0x0f0f0f0fu) | ((u << 4) & 0xf0f0f0f0u);
+    a[i + 1] = ((t >> 4) & 0x0f0f0f0fu) | (u & 0xf0f0f0f0u);
+  }
+}
+
 // What eight codes stand for
 __device__ __forceinline__ void kv4_values(unsigned int w, float s, float* o) {
   const f32x2 a[4] = {kv4_levels<0>(w), kv4_levels<1>(w), kv4_levels<2>(w), kv4_levels<3>(w)};

@@ -13,6 +13,7 @@ struct Kv4Params {
   Kv4View c;
   int L, kv_heads, tile0;
   int own_lo, own_n, own_period;               // as AttnArgs
+  unsigned int period_recip;
 };
 
 // Largest bits over the G lanes of a row
@@ -44,7 +45,7 @@ __device__ __forceinline__ unsigned int encode8(const float* x, float s, float i
 __device__ __forceinline__ long long own_row(const Kv4Params& p, int j) {
   if (j >= p.L) return -1;
   if (p.own_period > 0) {
-    const int r = j / p.own_period, rel = j - r * p.own_period - p.own_lo;
+    const int r = (int)quotient_u32((unsigned int)j, (unsigned int)p.own_period, p.period_recip), rel = j - r * p.own_period - p.own_lo;
     return rel >= 0 && rel < p.own_n ? (long long)r * p.own_n + rel : -1;
   }
   const int rel = j - p.own_lo;
@@ -58,7 +59,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_refresh_kernel(Kv4Params p) {
   constexpr int G = D / 8, ROWS = 256 / G, PASS = 64 / ROWS, PITCH = G + 1;
   __shared__ unsigned int vw[64 * PITCH];
-  __shared__ unsigned char mine[64];
+  __shared__ __attribute__((aligned(8))) unsigned char mine[64];
   const int tid = threadIdx.x, sub = tid % G, row = tid / G;
   const int tile = p.tile0 + blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const long long head = (long long)b * p.kv_heads + h;
@@ -79,6 +80,8 @@ __global__ __launch_bounds__(256) void kv4_refresh_kernel(Kv4Params p) {
 #pragma unroll
   for (int i = 0; i < PASS; ++i) {
     const int r = i * ROWS + row;
+    if (sub == 0) mine[r] = from[i] >= 0;
+    if (__builtin_amdgcn_ballot_w64(from[i] >= 0) == 0) continue;          // a strip of columns: most waves' rows are another patch's
     const long long at = head * p.c.pitch + (long long)tile * 64 + r;
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
@@ -94,28 +97,30 @@ __global__ __launch_bounds__(256) void kv4_refresh_kernel(Kv4Params p) {
       if (kv == 1) vw[r * PITCH + sub] = w;
       if (sub == 0 && from[i] >= 0) (kv ? p.c.vs : p.c.ks)[at] = (bf16_t)(__float_as_uint(s) >> 16);
     }
-    if (sub == 0) mine[r] = from[i] >= 0;
   }
   __syncthreads();
   unsigned char* vt = p.c.vc + (head * (p.c.pitch / 64) + tile) * (D * 32);
+  if (tid >= D) return;
+  const int g = tid >> 3, o = tid & 7;                     // values 8 g .., keys 8 o ..
+  const u32x2 of = *reinterpret_cast<const u32x2*>(mine + 8 * o);
+  if (!(of.x | of.y)) return;
+  unsigned int w[8];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) {                       // dword o of value e: keys 8 o ..
-    const int idx = i * 256 + tid, e = idx >> 3, o = idx & 7;
-    unsigned int w = 0, own = 0;
+  for (int j = 0; j < 8; ++j) w[j] = vw[(8 * o + j) * PITCH + g];
+  kv4_turn(w);
+  if ((of.x & of.y) == 0x01010101u) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w |= ((vw[(8 * o + j) * PITCH + (e >> 3)] >> (4 * (e & 7))) & 15u) << (4 * j);
-      own |= (unsigned int)mine[8 * o + j] << j;
-    }
-    unsigned char* dst = vt + e * 32 + o * 4;
-    if (own == 0xffu) {
-      *reinterpret_cast<unsigned int*>(dst) = w;
-    } else if (own) {
+    for (int e = 0; e < 8; ++e) *reinterpret_cast<unsigned int*>(vt + (8 * g + e) * 32 + o * 4) = w[e];
+    return;
+  }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const unsigned int o2 = (own >> (2 * j)) & 3u, keep = o2 == 3u ? 0u : o2 == 1u ? 0xf0u : 0x0fu;
-        if (o2) dst[j] = (unsigned char)((((w >> (8 * j)) & 0xffu) & ~keep) | (keep ? dst[j] & keep : 0u));
-      }
+  for (int j = 0; j < 4; ++j) {                            // keys 2 j and 2 j + 1
+    const unsigned int o2 = ((j < 2 ? of.x : of.y) >> (16 * (j & 1))) & 0x101u, keep = o2 == 0x101u ? 0u : o2 == 1u ? 0xf0u : 0x0fu;
+    if (!o2) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      unsigned char* dst = vt + (8 * g + e) * 32 + o * 4 + j;
+      *dst = (unsigned char)((((w[e] >> (8 * j)) & 0xffu) & ~keep) | (keep ? *dst & keep : 0u));
     }
   }
 }
@@ -128,13 +133,9 @@ __device__ __forceinline__ void turn_values(const unsigned char* vt, unsigned in
     unsigned int src[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) src[e] = *reinterpret_cast<const unsigned int*>(vt + (8 * g + e) * 32 + o * 4);
+    kv4_turn(src);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      unsigned int w = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w |= ((src[e] >> (4 * j)) & 15u) << (4 * e);
-      vw[(8 * o + j) * (D / 8 + 1) + g] = w;
-    }
+    for (int j = 0; j < 8; ++j) vw[(8 * o + j) * (D / 8 + 1) + g] = src[j];
   }
 }
 
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(Kv4Params p, const int*
     if (j >= p.L || own_row(p, j) >= 0) continue;
     int before = j - p.own_lo;                             // of the patch's rows, how many come before row j
     if (p.own_period > 0) {
-      const int q = j / p.own_period;
+      const int q = (int)quotient_u32((unsigned int)j, (unsigned int)p.own_period, p.period_recip);
       before = q * p.own_n + (j - q * p.own_period >= p.own_lo ? p.own_n : 0);
     } else {
       before = before >= 0 ? p.own_n : 0;
@@ -220,6 +221,7 @@ int launch_kv4_expand(const Kv4Args& a, const int* lens, long long rows, void* k
   p.ko = k; p.vo = v;
   p.c = kv4_view(a.cache, a.B, a.L, a.kv_heads, a.d);
   p.L = a.L; p.kv_heads = a.kv_heads; p.own_lo = a.own_lo; p.own_n = a.own_n; p.own_period = a.own_period;
+  p.period_recip = a.own_period > 0 ? reciprocal_u32((unsigned int)a.own_period) : 0u;
   const dim3 grid((unsigned)(p.c.pitch / 64), (unsigned)a.kv_heads, (unsigned)a.B);
   if (a.d == 64) hipLaunchKernelGGL(kv4_expand_kernel<64>, grid, dim3(256), 0, st, p, lens, rows);
   else hipLaunchKernelGGL(kv4_expand_kernel<128>, grid, dim3(256), 0, st, p, lens, rows);
@@ -232,6 +234,7 @@ int launch_kv4_refresh(const Kv4Args& a, hipStream_t st) {
   p.k = a.k; p.v = a.v; p.ldk = a.ldk; p.bsk = a.bsk; p.ldv = a.ldv; p.bsv = a.bsv;
   p.c = kv4_view(a.cache, a.B, a.L, a.kv_heads, a.d);
   p.L = a.L; p.kv_heads = a.kv_heads; p.own_lo = a.own_lo; p.own_n = a.own_n; p.own_period = a.own_period;
+  p.period_recip = a.own_period > 0 ? reciprocal_u32((unsigned int)a.own_period) : 0u;
   const int last = a.own_period > 0 ? a.L - 1 : a.own_lo + a.own_n - 1;
   p.tile0 = a.own_period > 0 ? 0 : a.own_lo / 64;
   const dim3 grid((unsigned)(last / 64 - p.tile0 + 1), (unsigned)a.kv_heads, (unsigned)a.B);
