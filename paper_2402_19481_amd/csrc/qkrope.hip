@@ -49,11 +49,11 @@ __device__ __forceinline__ void st_n(bf16_t* p, const float (&v)[4]) {
   *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
 }
 
-// G lanes share a head's row, V values each; a wave takes `steps` times 64 / G heads of one token, so the token's angles and the scales are
-// read once.  HALVES: value i turns with value i + half (the partner's vector is read as well, from L1); else with its neighbour.
+// G lanes share a head's row, V values each; a wave takes `steps` (at most four) times 64 / G heads of one token, so the token's angles and the scales are
+// read once.  HALVES: value i turns with value i + half, which another lane of the row has normed; else with its neighbour.
 template <typename T, int V, int G, bool NORM, bool HALVES>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p) {
-  constexpr int U = 4;                                     // rows of a lane in flight
+  constexpr int U = 4;                                     // rows of a lane, at most
   const unsigned int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (w >= p.waves) return;
   const int lane = threadIdx.x & 63, sub = lane / G, e0 = (lane % G) * V;
@@ -90,62 +90,54 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p) {
       }
     }
   }
-  const int pair = HALVES && turns ? (e0 >= p.half ? -p.half : p.half) : 0;   // where the partner's vector lies
+  const int partner = HALVES && turns ? 4 * (lane + (e0 >= p.half ? -p.half : p.half) / V) : 4 * lane;   // the lane of the other half's values
 
-  for (int u0 = 0; u0 < p.steps; u0 += U) {
-    float x[U][V], y[HALVES ? U : 1][V];
+  // all that the wave reads is requested at once
+  float x[U][V], gx[NORM ? U : 1][V];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = (first + u0 + u) * (64 / G) + sub;
+  for (int u = 0; u < U; ++u) {
+    const int h = (first + u) * (64 / G) + sub;
 #pragma unroll
-      for (int i = 0; i < V; ++i) { x[u][i] = 0.f; if constexpr (HALVES) y[u][i] = 0.f; }
-      if (u0 + u < p.steps && in && h < p.heads) {
-        const T* src = h < p.hq ? (const T*)p.q + b * p.bsq + t * p.ldq + (long long)h * p.d : (const T*)p.k + b * p.bsk + t * p.ldk + (long long)(h - p.hq) * p.d;
-        ld_n(src + e0, x[u]);
-        if constexpr (HALVES) ld_n(src + e0 + pair, y[u]);
-      }
+    for (int i = 0; i < V; ++i) {
+      x[u][i] = 0.f;
+      if constexpr (NORM) gx[u][i] = 1.f;
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u0 + u >= p.steps) break;
-      const int h = (first + u0 + u) * (64 / G) + sub;
+    if (u < p.steps && in && h < p.heads) {
       const bool isq = h < p.hq;
+      const T* src = isq ? (const T*)p.q + b * p.bsq + t * p.ldq + (long long)h * p.d : (const T*)p.k + b * p.bsk + t * p.ldk + (long long)(h - p.hq) * p.d;
+      ld_n(src + e0, x[u]);
       if constexpr (NORM) {
-        float sq = 0.f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) sq = fmaf(x[u][i], x[u][i], sq);
-        const float v = fmaf(group_sum<G>(sq), p.inv_d, p.eps);
-        float r = __builtin_amdgcn_rsqf(v);
-        r = fmaf(0.5f * r, fmaf(-v * r, r, 1.f), r);       // (the instruction is off by one unit in the last place)
         const float* g = isq ? p.qg : p.kg;
-        if (g && in) {
+        if (g) {
 #pragma unroll
-          for (int i = 0; i < V; i += 4) {
-            float t4[4];
-            ld_vec(g + e0 + i, t4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[u][i + j] *= r * t4[j];
-            if constexpr (HALVES) {
-              ld_vec(g + e0 + pair + i, t4);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) y[u][i + j] *= r * t4[j];
-            }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i) { x[u][i] *= r; if constexpr (HALVES) y[u][i] *= r; }
+          for (int i = 0; i < V; i += 4) ld_vec(g + e0 + i, gx[u] + i);
         }
       }
-      float o[V];
+    }
+  }
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float other = HALVES ? y[HALVES ? u : 0][i] : x[u][i ^ 1];
-        o[i] = turns ? fmaf(x[u][i], c[i], other * s[i]) : x[u][i];
-      }
-      if (in && h < p.heads) {
-        T* dst = isq ? (T*)p.qo + b * p.bsqo + t * p.ldqo + (long long)h * p.d : (T*)p.ko + b * p.bsko + t * p.ldko + (long long)(h - p.hq) * p.d;
-        st_n(dst + e0, o);
-      }
+  for (int u = 0; u < U; ++u) {
+    if (u >= p.steps) break;
+    const int h = (first + u) * (64 / G) + sub;
+    if constexpr (NORM) {
+      float sq = 0.f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) sq = fmaf(x[u][i], x[u][i], sq);
+      const float v = fmaf(group_sum<G>(sq), p.inv_d, p.eps);
+      float r = __builtin_amdgcn_rsqf(v);
+      r = fmaf(0.5f * r, fmaf(-v * r, r, 1.f), r);         // (the instruction is off by one unit in the last place)
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[u][i] *= r * gx[u][i];
+    }
+    float o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float other = HALVES ? __int_as_float(__builtin_amdgcn_ds_bpermute(partner, __float_as_int(x[u][i]))) : x[u][i ^ 1];
+      o[i] = turns ? fmaf(x[u][i], c[i], other * s[i]) : x[u][i];
+    }
+    if (in && h < p.heads) {
+      T* dst = h < p.hq ? (T*)p.qo + b * p.bsqo + t * p.ldqo + (long long)h * p.d : (T*)p.ko + b * p.bsko + t * p.ldko + (long long)(h - p.hq) * p.d;
+      st_n(dst + e0, o);
     }
   }
 }
