@@ -167,21 +167,36 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
 
   // A block of rows (or the share's part of one)
   struct Block { int kh, b, row0, lo, nt, n0, tiles0; bool whole; };
+  int lo0 = (int)(pos % sh.tiles), rb, kh0, b0, n00;       // of the next one: its first tile, place, keys of segment 0
+  {
+    const unsigned int block = pos / sh.tiles, bh = block / (unsigned int)nrb;
+    rb = (int)(block - bh * nrb);
+    b0 = (int)(bh / (unsigned int)p.kv_heads);
+    kh0 = (int)(bh - (unsigned int)b0 * p.kv_heads);
+    n00 = b0 < p.B ? seg0_rows(p, b0) : 0;
+  }
   auto open = [&]() DF_INLINE {
     Block r;
-    const unsigned int block = pos / sh.tiles;
-    r.lo = (int)(pos - block * sh.tiles);
+    r.lo = lo0;
     int hi = (int)(r.lo + end - pos < sh.tiles ? r.lo + end - pos : sh.tiles);
     pos += hi - r.lo;
     r.whole = r.lo == 0 && hi == (int)sh.tiles;
-    const int bh = (int)(block / (unsigned int)nrb);
-    r.row0 = ((int)(block % (unsigned int)nrb)) * BLK + wave * 32 * QB;
-    r.b = bh / p.kv_heads;
-    r.kh = bh - r.b * p.kv_heads;
-    r.n0 = seg0_rows(p, r.b);
+    r.row0 = rb * BLK + wave * 32 * QB;
+    r.b = b0;
+    r.kh = kh0;
+    r.n0 = n00;
     r.tiles0 = (r.n0 + 63) >> 6;
     if (hi > r.tiles0 + ((p.seg[1].n + 63) >> 6)) hi = r.tiles0 + ((p.seg[1].n + 63) >> 6);
     r.nt = hi > r.lo ? hi - r.lo : 0;
+    lo0 = 0;
+    if (++rb == nrb) {
+      rb = 0;
+      if (++kh0 == p.kv_heads) {
+        kh0 = 0;
+        ++b0;
+        if (pos < end) n00 = seg0_rows(p, b0);
+      }
+    }
     return r;
   };
   bf16x8 qreg[QB][KS], qnext[QB][KS];
