@@ -200,19 +200,54 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
     return r;
   };
   bf16x8 qreg[QB][KS], qnext[QB][KS];
-  auto queries = [&](const Block& k) DF_INLINE {           // the wave's rows of Q -> qnext
+  auto queries = [&](const Block& k) DF_INLINE {           // the wave's rows of Q -> qnext (behind the last row it is read again, and not used)
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
-      const bool have = k.row0 + 32 * n + c < p.rows;
-      const bf16_t* qp = (const bf16_t*)p.q + row_offset(p, k.b, k.kh, have ? k.row0 + 32 * n + c : 0, p.bsq, p.ldq);
+      const int row = k.row0 + 32 * n + c;
+      const bf16_t* qp = (const bf16_t*)p.q + row_offset(p, k.b, k.kh, row < p.rows ? row : p.rows - 1, p.bsq, p.ldq);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        u32x4 t = {0u, 0u, 0u, 0u};
-        if (have && 16 * s + 8 * g < p.d) t = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * g);
-        qnext[n][s] = __builtin_bit_cast(bf16x8, t);
-      }
+      for (int s = 0; s < KS; ++s)
+        qnext[n][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + (p.d == D || 16 * s + 8 * g < p.d ? 16 * s + 8 * g : 0)));
     }
   };
+  // What is loaded next: the rows of a tile's K and V, the keys and the tiles from it on in its segment (and the block's tiles in segment 1 behind
+  // it), all in scalar registers; and what was loaded before: the keys (and 256 if segment 1's) of tiles t .. t + 2 of an iteration, V of t + 1, t + 2.
+  const char *fk = nullptr, *fv = nullptr, *v1 = nullptr, *v2 = nullptr;
+  long long kstep = 0, vstep = 0;
+  int left = 0, tiles = 0, rest = 0, w0 = 0, w1 = 0, w2 = 0, kw = 0, vw = 0;
+  bool second = false, beyond = false;                     // ... is segment 1's; is in the next block
+  unsigned int kofs[LPT], vofs[LPT];                       // a lane's offsets in a tile of kw and vw keys
+  auto feed = [&](int kh, int b, int z, int tile, int n, int count) DF_INLINE {
+    const Seg& s = p.seg[z];
+    kstep = 128 * s.ldk; vstep = 128 * s.ldv;
+    fk = (const char*)s.k + 2 * ((long long)b * s.bsk + (long long)kh * s.hsk) + tile * kstep;
+    fv = (const char*)s.v + 2 * ((long long)b * s.bsv + (long long)kh * s.hsv) + tile * vstep;
+    left = n - tile * 64; tiles = count; second = z;
+  };
+  auto feed_block = [&](const Block& k) DF_INLINE {
+    const int kh = k.kh, b = k.b, lo = k.lo, nt = k.nt, n0 = k.n0, tiles0 = k.tiles0;
+    if (lo < tiles0) {
+      const int some = tiles0 - lo < nt ? tiles0 - lo : nt;
+      feed(kh, b, 0, lo, n0, some);
+      rest = nt - some;
+    } else {
+      feed(kh, b, 1, lo - tiles0, p.seg[1].n, nt);
+      rest = 0;
+    }
+  };
+  auto offsets = [&](auto isv, int word, unsigned int (&ofs)[LPT]) DF_INLINE {
+    constexpr bool V = decltype(isv)::value;
+    const Seg& s = p.seg[word >> 8];
+    const int ld = (int)(V ? s.ldv : s.ldk), last = (word & 255) - 1;
+#pragma unroll
+    for (int j = 0; j < LPT; ++j) {                        // behind the last key its row is read again: the weight is 0, the value must be finite
+      ofs[j] = 2u * (unsigned int)((trow[j] < last ? trow[j] : last) * ld) + (V ? vch[j] : kch[j]);   // where the others are
+      asm volatile("" : "+v"(ofs[j]));
+    }
+  };
+  auto load = [&](const char* base, const unsigned int (&ofs)[LPT], int j, int to) DF_INLINE { lds_load16(base, ofs[j], smem + to + 1024 * j); };
+  using IsK = std::false_type;
+  using IsV = std::true_type;
 
   Block blk = open(), after = blk;
   bool primed = false;                                     // the last block's final iterations have requested this one's first tiles and Q
@@ -234,46 +269,8 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
       for (int s = 0; s < KS; ++s) {
         qreg[n][s] = qnext[n][s];
         asm volatile("" : "+v"(qreg[n][s]));               // Q has arrived: the loop does not wait for it, with the direct loads
+        if (p.d != D && 16 * s + 8 * g >= p.d) qreg[n][s] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
       }
-
-    // Tile i and which of its keys count.  Past the end: the next block's, or the last one again, which keeps the counts of loads in
-    // flight uniform.
-    struct Info { int t; bool next; unsigned long long w; };
-    auto info = [&](int i) DF_INLINE {
-      Info r;
-      r.next = i >= nt && ahead;
-      if (i >= nt) i = !ahead ? nt - 1 : i - nt < ant ? i - nt : ant - 1;
-      const int z0 = r.next ? after.tiles0 : tiles0;
-      r.t = (r.next ? after.lo : lo) + i;
-      r.w = r.t < z0 ? low_bits((r.next ? after.n0 : n0) - r.t * 64) : low_bits(n1 - (r.t - z0) * 64);
-      return r;
-    };
-    // Where the wave's loads of a tile come from.  Rows behind the last key are read as one that is: their weight is 0, the value must be finite
-    // where the others are.
-    struct Source { const char* base; unsigned int ofs[LPT]; };
-    auto source = [&](auto isv, const Info& i) DF_INLINE {
-      constexpr bool V = decltype(isv)::value;
-      const int z0 = i.next ? after.tiles0 : tiles0;
-      const bool second = i.t >= z0;
-      const Seg& s = p.seg[second ? 1 : 0];
-      const int ld = (int)(V ? s.ldv : s.ldk);
-      Source r;
-      r.base = (const char*)((const bf16_t*)(V ? s.v : s.k) + (long long)(i.next ? after.b : b) * (V ? s.bsv : s.bsk) +
-                             (long long)(i.next ? after.kh : kh) * (V ? s.hsv : s.hsk) + (long long)(second ? i.t - z0 : i.t) * 64 * ld);
-      const bool full = i.w == ~0ULL;
-      const int some = __builtin_ctzll(i.w);
-      const unsigned int mine = (unsigned int)(i.w >> (16 * wave));       // (a wave's loads cover 16 rows of the tile)
-#pragma unroll
-      for (int j = 0; j < LPT; ++j) {
-        const int from = full || (mine >> (trow[j] & 15) & 1) ? trow[j] : some;
-        r.ofs[j] = 2u * (unsigned int)(from * ld) + (V ? vch[j] : kch[j]);
-        asm volatile("" : "+v"(r.ofs[j]));
-      }
-      return r;
-    };
-    auto load = [&](const Source& f, int j, int to) DF_INLINE { lds_load16(f.base, f.ofs[j], smem + to + 1024 * j); };
-    using IsK = std::false_type;
-    using IsV = std::true_type;
 
     f32x16 o[QB][DB], sa[QB][2];
     u32x4 pk[QB][4];
@@ -307,8 +304,9 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
           for (int n = 0; n < QB; ++n) s_mfma(k, s, kb, n);
         }
     };
-    auto hide = [&](unsigned long long bits) DF_INLINE {             // scores of keys that are none
-      if (bits == ~0ULL) return;
+    auto hide = [&](int word) DF_INLINE {                            // scores behind the last key
+      if ((word & 255) == 64) return;
+      const unsigned long long bits = low_bits(word & 255);
       const unsigned long long mine = bits >> (8 * g);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -341,8 +339,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
 
     // Iteration t: weights of tile t from the scores in sa, O += V P of tile t - 1 (PV), S of tile t + 1.  Sixteen slots of M * QB matrix
     // instructions and their share of the vector instructions; operands are read from LDS some slots ahead.
-    Info cur, n1i, n2i, n3i;
-    Source ka, va;                                         // of K_{t+3} and V_{t+1}
+    const char *ka = nullptr, *va = nullptr;               // of K_{t+3} and V_{t+1}
     float tsum[QB];
     int x = 0;                                             // slot of tile t + 1; tile t - 1's, which tile t + 3 takes, is two from it
     auto tile = [&](auto pvc) DF_INLINE {
@@ -400,20 +397,20 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
         if (i + A < 16) fetch(i + A);
         switch (i) {
           case 0: E(0, 0); break;
-          case 1: E(0, 1); load(ka, 0, kd); break;
-          case 2: C(0); load(ka, 1, kd); break;
+          case 1: E(0, 1); load(ka, kofs, 0, kd); break;
+          case 2: C(0); load(ka, kofs, 1, kd); break;
           case 3: E(1, 0); break;
           case 4: E(1, 1); break;
           case 5: C(1); S(0); break;
-          case 6: E(2, 0); if constexpr (LPT > 2) load(ka, 2, kd); break;
+          case 6: E(2, 0); if constexpr (LPT > 2) load(ka, kofs, 2, kd); break;
           case 7: E(2, 1); S(1); break;
-          case 8: C(2); load(va, 0, vd); break;
+          case 8: C(2); load(va, vofs, 0, vd); break;
           case 9: E(3, 0); break;
-          case 10: E(3, 1); load(va, 1, vd); break;
-          case 11: S(2); if constexpr (LPT > 2) load(ka, 3, kd); break;
-          case 12: C(3); if constexpr (LPT > 2) load(va, 2, vd); break;
+          case 10: E(3, 1); load(va, vofs, 1, vd); break;
+          case 11: S(2); if constexpr (LPT > 2) load(ka, kofs, 3, kd); break;
+          case 12: C(3); if constexpr (LPT > 2) load(va, vofs, 2, vd); break;
           case 13: S(3); break;
-          case 14: if constexpr (LPT > 2) load(va, 3, vd); break;
+          case 14: if constexpr (LPT > 2) load(va, vofs, 3, vd); break;
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -425,7 +422,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
       for (int n = 0; n < QB; ++n) redo |= __builtin_amdgcn_ballot_w64(tsum[n] > kRedo) != 0;
       if (redo) {
         scores(t);
-        hide(cur.w);
+        hide(w0);
 #pragma unroll
         for (int n = 0; n < QB; ++n) {
           scale_by(n, settle(n));
@@ -463,36 +460,69 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
     };
 
     if (nt > 0) {
-      cur = info(0); n1i = info(1); n2i = info(2); n3i = info(3);
+      // The next tile to load; past the block's end the next block's, or the last one again, which keeps the counts of loads in flight uniform
+      int w3 = 0;
+      const char* v3 = nullptr;
+      auto take = [&]() DF_INLINE {
+        if (tiles == 0) {
+          if (rest > 0) {
+            const Block& of = beyond ? after : blk;
+            const int kh1 = of.kh, b1 = of.b, some = rest;
+            feed(kh1, b1, 1, 0, n1, some);
+            rest = 0;
+          } else if (!beyond && ahead) {
+            feed_block(after);
+            beyond = true;
+          }
+        }
+        if (tiles > 0) {
+          ka = fk; v3 = fv;
+          w3 = (left < 64 ? left : 64) | (second ? 256 : 0);
+          fk += kstep; fv += vstep;
+          left -= 64; --tiles;
+        } else {
+          ka = fk - kstep; v3 = v2; w3 = w2;
+        }
+        if (w3 != kw) { kw = w3; offsets(IsK{}, w3, kofs); }
+      };
+      auto next = [&]() DF_INLINE { w0 = w1; w1 = w2; w2 = w3; v1 = v2; v2 = v3; };
       if (!primed) {
         s0 = 0;
+        kw = vw = 0;
+        beyond = false;
+        feed_block(blk);
         block_sync();                                      // (every wave's reads of the last block are done: they were waited for)
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
-          ka = source(IsK{}, i == 0 ? cur : i == 1 ? n1i : n2i);
+          take();
 #pragma unroll
-          for (int j = 0; j < LPT; ++j) load(ka, j, slot_of(i) + wofs);
+          for (int j = 0; j < LPT; ++j) load(ka, kofs, j, slot_of(i) + wofs);
+          if (i == 0) {
+            va = v3;
+            vw = w3;
+            offsets(IsV{}, vw, vofs);
+          }
+          next();
         }
-        va = source(IsV{}, cur);
 #pragma unroll
-        for (int j = 0; j < LPT; ++j) load(va, j, VR + wofs);
+        for (int j = 0; j < LPT; ++j) load(va, vofs, j, VR + wofs);
         sync_tile();
       }
-      auto next = [&](int t) DF_INLINE { cur = n1i; n1i = n2i; n2i = n3i; n3i = info(t + 4); };
       // an iteration's loads, and at the last one the next block's Q
       auto begin = [&](int t) DF_INLINE {
-        ka = source(IsK{}, n3i);
-        va = source(IsV{}, n1i);
+        take();
+        va = v1;
+        if (w1 != vw) { vw = w1; offsets(IsV{}, vw, vofs); }
         if (t == nt - 1 && ahead) queries(after);
       };
       if (idle) {
         for (int t = 0; t < nt; ++t) {
           begin(t);
 #pragma unroll
-          for (int j = 0; j < LPT; ++j) load(ka, j, slot_of(s0 + t + 3) + wofs);
+          for (int j = 0; j < LPT; ++j) load(ka, kofs, j, slot_of(s0 + t + 3) + wofs);
 #pragma unroll
-          for (int j = 0; j < LPT; ++j) load(va, j, VR + slot_of(s0 + t + 1) + wofs);
-          next(t);
+          for (int j = 0; j < LPT; ++j) load(va, vofs, j, VR + slot_of(s0 + t + 1) + wofs);
+          next();
           sync_tile();
         }
       } else {
@@ -506,7 +536,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
           sync_tile();
         };
         scores(0);
-        hide(cur.w);
+        hide(w0);
 #pragma unroll
         for (int n = 0; n < QB; ++n) settle(n);
         begin(0);
@@ -515,37 +545,34 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
 #pragma unroll
         for (int n = 0; n < QB; ++n) l[n] += tsum[n];      // (weights of at most 1)
         x = slot_of(s0 + 2);
-        next(0);
+        next();
         sync_tile();
         int t = 1;
         while (t < nt) {
-          // Tiles t .. t + 3 whole and of one segment: as long as that holds.  (Without a scope of their own its values spill, 400 bytes of them.)
+          // Tiles t .. t + 3 whole and of one segment: as long as that holds.  (Without a scope of their own its values spill.)
           {
-            const int second = lo + t >= tiles0;
-            int run = (second ? tiles0 + (n1 >> 6) : n0 >> 6) - lo;
-            if (run > nt) run = nt;
-            if (t + 3 < run) {
-              const Seg& s = p.seg[second];
-              const long long kstep = 128 * s.ldk, vstep = 128 * s.ldv;
-              ka = source(IsK{}, info(t + 3));
-              va = source(IsV{}, info(t + 1));
-              cur.w = ~0ULL;
+            int run = tiles < left >> 6 ? tiles : left >> 6;
+            if (run > nt - 1 - t) run = nt - 1 - t;
+            const int whole = second ? 320 : 64;
+            if (run > 0 && w0 == whole && w1 == whole && w2 == whole && kw == whole && vw == whole) {
+              left -= 64 * run; tiles -= run;
+              const int to = t + run;
               do {
+                ka = fk; va = v1;
                 tile(std::true_type{});
-                ka.base += kstep;
-                va.base += vstep;
+                v1 = v2; v2 = fv;
+                fk += kstep; fv += vstep;
                 finish(t);
                 ++t;
-              } while (t + 3 < run);
-              cur = info(t); n1i = info(t + 1); n2i = info(t + 2); n3i = info(t + 3);
+              } while (t < to);
               continue;
             }
           }
           begin(t);
-          hide(cur.w);
+          hide(w0);
           tile(std::true_type{});
           finish(t);
-          next(t);
+          next();
           ++t;
         }
         const int vt = slot_of(s0 + nt - 1);
@@ -564,6 +591,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
       s0 = (s0 + nt) & 3;
     }
     primed = ahead;
+    beyond = false;
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
       if (row0 + 32 * n + c >= p.rows) continue;
@@ -572,22 +600,23 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
       const int at0 = wave * 32 * QB + 32 * n + c;
       bf16_t* op = (bf16_t*)p.out + row_offset(p, b, kh, row0 + 32 * n + c, (long long)p.Lq * p.kv_heads * p.group * p.d, (long long)p.kv_heads * p.group * p.d);
       float* po = p.part_o + ((long long)slot * BLK + at0) * p.d;
+      auto store = [&](int db, int f) DF_INLINE {
+        const int at = 32 * db + 16 * f + 8 * g;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = o[n][db][8 * f + e] * inv;
+        if (whole) {
+          st_vec(op + at, v);
+        } else {
+          st_vec(po + at, v);
+          st_vec(po + at + 4, v + 4);
+        }
+      };
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          const int at = 32 * db + 16 * f + 8 * g;
-          if (at >= p.d) continue;
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = o[n][db][8 * f + e] * inv;
-          if (whole) {
-            st_vec(op + at, v);
-          } else {
-            st_vec(po + at, v);
-            st_vec(po + at + 4, v + 4);
-          }
-        }
+        for (int f = 0; f < 2; ++f)
+          if (p.d == D || 32 * db + 16 * f + 8 * g < p.d) store(db, f);
       if (!whole && g == 0) {
         float* ml = p.part_ml + 2 * ((long long)slot * BLK + at0);
         ml[0] = nt > 0 ? m[n] : -INFINITY;
@@ -1384,8 +1413,9 @@ double plan_held(const Task& k, long long ns, int nw, Plan& r) {
          (r.nsplit > 1 ? merge_us((double)r.nsplit * heads * k.rows, k.d) : 0.0);
 }
 
-// The pipelined form with `qb` blocks of 32 rows a wave.  A tile takes a workgroup 0.85 us, two on a unit 1.16 (128 values 1.1; 256 rows 1.05, one on a
-// unit); its code is long, the first pass over it costs.
+// The pipelined form with `qb` blocks of 32 rows a wave.  A tile takes a workgroup 0.85 us, two on a unit 1.16 (128 values 1.1; 256 rows 1.1, one on a
+// unit, and beginning and end of a block cost more: 1200 queries on 10240 keys 55 us with 128 rows, 57 with 256; 7200 on 1280 49 and 52, on 5120 124
+// and 125, on 57600 of a cache 1260 and 1185); its code is long, the first pass over it costs.
 double plan_rows(const Task& k, int qb, Plan& r) {
   r = Plan{};
   r.ok = true;
@@ -1412,8 +1442,8 @@ double plan_rows(const Task& k, int qb, Plan& r) {
     r.parts = (size_t)n * 2 * r.block * (k.d + 2) * sizeof(float);
   }
   const bool two = fit == 512 && s.count > 256;
-  const double tile = k.d > 64 ? 1.1 : qb == 2 ? 1.05 : two ? 1.16 : 0.85;
-  return (k.d > 64 || qb == 2 ? 7.7 : 6.2) + tile * (double)(s.per + 1) * (double)((s.count + fit - 1) / fit) +
+  const double tile = k.d > 64 ? 1.1 : qb == 2 ? 1.1 : two ? 1.16 : 0.85;
+  return (qb == 2 ? 12.0 : k.d > 64 ? 7.7 : 6.2) + tile * (double)(s.per + 1) * (double)((s.count + fit - 1) / fit) +
          (r.parts ? merge_us(1.2 * (double)s.count * r.block, k.d) : 0.0) + (k.cached || k.masked ? 4.0 + (double)(heads * keys0) * k.d * (k.cached ? 4.5 : 8.0) / 4e6 : 0.0);
 }
 
