@@ -1463,6 +1463,26 @@ double plan_float(const Task& k, int kw, long long ns, Plan& r) {
   return 4.5 + tile * (double)(((wgs + 255) / 256) * each) + (r.nsplit > 1 ? merge_us((double)r.nsplit * heads * k.rows, k.d) : 0.0);
 }
 
+// Few rows against the cache as it is: 1.05 us per 1000 tiles and blocks of 32 rows (128 values 1.2).  10 heads of 64, 57600 keys: 64 rows 35 us
+// (held 75), 128 rows 47 (78), 256 rows 76 (94), 512 rows 153 (pipelined 138); 4 x 20 heads, 1024 keys: 128 rows 18 (21), 512 rows 26 (40).
+double plan_few(const Task& k, Plan& r) {
+  r = Plan{};
+  r.ok = true;
+  const long long heads = (long long)k.B * k.kv_heads, tiles = (k.L + 63) / 64;
+  r.kind = kFewKv4; r.nq = k.rows > 16 ? 2 : 1; r.block = 16 * r.nq; r.tile = 64;
+  const long long blocks = heads * ((k.rows + r.block - 1) / r.block);
+  long long ns = 1;
+  if (blocks < 768) ns = 768 / blocks;
+  if (ns > tiles / 4) ns = tiles / 4;
+  if (ns < 1) ns = 1;
+  if (ns > 64) ns = 64;
+  r.tiles_per_split = (int)((tiles + ns - 1) / ns);
+  r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
+  if (blocks * r.nsplit > 0x7fffffffLL) return 1e30;
+  if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * k.rows * (k.d + 2) * sizeof(float);
+  return 6.0 + (k.d == 64 ? 1.05e-3 : 1.2e-3) * (double)(blocks * tiles) + (r.nsplit > 1 ? merge_us((double)r.nsplit * heads * k.rows, k.d) : 0.0);
+}
+
 Plan choose(const Task& k) {
   Plan r = {};
   r.ok = true;
@@ -1485,22 +1505,13 @@ Plan choose(const Task& k) {
     if (best >= 1e29) r.ok = false;
     return r;
   }
-  if (k.cached && own == 0 && rows <= 64) {
-    r.kind = kFewKv4; r.nq = rows > 16 ? 2 : 1; r.block = 16 * r.nq; r.tile = 64;
-    const long long tiles = (k.L + 63) / 64, blocks = heads * ((rows + r.block - 1) / r.block);
-    long long ns = 1;
-    if (blocks < 768) ns = 768 / blocks;
-    if (ns > tiles / 4) ns = tiles / 4;
-    if (ns < 1) ns = 1;
-    if (ns > 64) ns = 64;
-    r.tiles_per_split = (int)((tiles + ns - 1) / ns);
-    r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
-    if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * rows * (k.d + 2) * sizeof(float);
+  const char* form = tune_env("DF_QATTN");
+  if (k.cached && own == 0 && (form ? !strcmp(form, "few") : rows <= 64)) {
+    plan_few(k, r);
     return r;
   }
   // The form that is predicted to take least
 #ifdef DF_TUNING
-  const char* form = tune_env("DF_QATTN");
   if (form && !strcmp(form, "rows1")) { plan_rows(k, 1, q); return q; }
   if (form && !strcmp(form, "rows2")) { plan_rows(k, k.d <= 64 ? 2 : 1, q); return q; }
 #endif
@@ -1515,6 +1526,7 @@ Plan choose(const Task& k) {
 #ifdef DF_TUNING
   if (form && !strcmp(form, "held") && best < 1e29) return r;
 #endif
+  if (k.cached && own == 0) offer(plan_few(k, q), q);
   offer(plan_rows(k, 1, q), q);
   if (k.d <= 64) offer(plan_rows(k, 2, q), q);
   if (best >= 1e29) r.ok = false;
