@@ -259,7 +259,8 @@ int df_cross_attn_packed(const void* xp, const void* wq_packed, const float* ln_
  *     Pair i of the first rot_dim values of a head is (2 i, 2 i + 1) if interleaved, else (i, i + rot_dim / 2):
  *     (a, b) -> (a cos - b sin, b cos + a sin).
  * d % 8 == 0, d <= 256; rot_dim % 8 == 0.  Addresses and strides: multiples of 16 bytes (float), 8 bytes (bf16; fastest with 16); gamma and rot
- * 16-byte aligned.  Sums are float: a row of values above 1e19 gives NaN.
+ * 16-byte aligned.  Sums are float: a row of values above 1e19 gives NaN.  B * T * ceil((heads + kv_heads) * lanes / 256) < 2^26 - 4, lanes = d / 8
+ * (float, or bf16 in multiples of 8 bytes: d / 4), rounded up to a power of two.
  */
 int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, void* q_out,
                     long long qo_ld, long long qo_bs, void* k_out, long long ko_ld, long long ko_bs, const float* q_gamma,
@@ -271,7 +272,7 @@ int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k
  * 64 values).  Each row (token, head) of d values is held as the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times a scale (of two equally near
  * ones 0, 1, 2 or 4), with sign; the scale is a sixth of the row's largest magnitude, rounded to six significant bits, so that what is held is
  * exact in bf16.  A row with an infinity or NaN is NaN as a whole, one below 2^-100 is zero.
- *   cache  device memory of df_kv4_bytes(B, L, kv_heads, d), 16-byte aligned, d 64 or 128 (0 for sizes it does not take); rows must be
+ *   cache  device memory of df_kv4_bytes(B, L, kv_heads, d), 16-byte aligned, d 64 or 128, L < 2^30 - 63 (0 for sizes it does not take); rows must be
  *          written before they are read, zeroed memory holds zeros.
  *   df_kv4_refresh  the rows of patch `patch_idx` of N of an H x W grid of tokens (L = H * W; split as in the *_axis functions) receive
  *          k, v [B, L / N, kv_heads, d], strides as above (16-byte multiples); one token of a sequence is patch t of N = L.  Other rows keep
@@ -293,8 +294,9 @@ int df_kv4_read(const void* cache, void* k, void* v, int B, int L, int kv_heads,
  *   df_attn_displaced_kv4  df_attn_displaced_axis with the stale rows in a cache: Lq = L / N queries, the patch's own rows from
  *                          k_fresh, v_fresh [B, L / N, kv_heads, d].
  *   df_cross_attn          k, v [B, Lk, kv_heads, d] of another length; d % 8 == 0, d <= 128.  key_mask [B, Lk]: 0 is no key; lens as above;
- *                          both may be NULL.  What k and v hold where there is no key does not matter, not even NaN.
- * Workspace: df_*_workspace_bytes of the same sizes (0: none needed, NULL will do, or sizes that are not taken), 256-byte aligned, the
+ *                          both may be NULL.  What k and v hold where there is no key does not matter, not even NaN;
+ *                          an infinite value of v under a key comes out infinite or NaN.
+ * Workspace: df_*_workspace_bytes of the same sizes (`masked`: whether there is a key_mask; 0: none needed, NULL will do, or sizes that are not taken), 256-byte aligned, the
  * caller's until the call's work is done; calls that overlap need workspaces of their own.  DF_ENOMEM if it is smaller.  Equal calls give
  * equal bits.
  */

@@ -336,7 +336,7 @@ int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k
 
 // Sizes of a 4-bit cache that the kernels take
 static inline bool kv4_sizes(long long B, long long L, int kv_heads, int d) {
-  return B > 0 && L > 0 && kv_heads > 0 && B <= 65535 && kv_heads <= 65535 && L <= 0x7fffffffLL - 63 && (d == 64 || d == 128);
+  return B > 0 && L > 0 && kv_heads > 0 && B <= 65535 && kv_heads <= 65535 && L <= (1LL << 30) - 64 && (d == 64 || d == 128);   // (launches: 32 bits of work items)
 }
 
 size_t df_kv4_bytes(int B, int L, int kv_heads, int d) { return kv4_sizes(B, L, kv_heads, d) ? kv4_bytes(B, L, kv_heads, d) : 0; }

@@ -88,7 +88,7 @@ __host__ __device__ inline unsigned int share_of(const Share& s, unsigned int ti
 // Where lengths (or the number of rows that a mask leaves) are known on the device only, the shares are those of the longest batch item: as many as
 // planned, of the keys there are.
 __device__ __forceinline__ Share share_of_keys(const QParams& p, Share s, int nrb) {
-  if (!p.lens) return s;
+  if (!p.lens || p.B > 1024) return s;                     // (of many batch items some have work while others have none)
   int longest = 0;
   for (int b = threadIdx.x & 63; b < p.B; b += 64) longest = max(longest, seg0_rows(p, b));
 #pragma unroll
@@ -125,8 +125,8 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
   }
   unsigned int pos = share_begin(sh, w);
   const unsigned int end = share_begin(sh, w + 1);
-  // Direct load j of the wave covers tile rows (LPT wave + j) * RPI + lane / CH; the chunks of a row are swizzled by it.  Values beyond d are read as
-  // the first ones (Q is 0 there, those of O are dropped).
+  // Direct load j of the wave covers tile rows (LPT wave + j) * RPI + lane / CH; the chunks of a row are swizzled by it.  (K and V have D
+  // values a row; where d is less they are zeros, Q is too, those of O are dropped.)
   unsigned int kch[LPT], vch[LPT];
   int trow[LPT];
 #pragma unroll
@@ -135,8 +135,8 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
     const int kc = (at ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 8;
     const int vc = (at ^ (D == 64 ? ((r >> 1) & 1) * 2 ^ ((r >> 3) & 1) * 4 : (r & 3) * 4)) * 8;
     trow[j] = r;
-    kch[j] = kc < p.d ? 2 * kc : 0;
-    vch[j] = vc < p.d ? 2 * vc : 0;
+    kch[j] = 2 * kc;
+    vch[j] = 2 * vc;
   }
   auto slot_of = [&](int i) DF_INLINE { return (i & 3) * TILE; };
   constexpr int VR = 4 * TILE;                             // the ring of V
@@ -681,47 +681,55 @@ __global__ __launch_bounds__(256) void merge_shares(QParams p, Share planned, in
   st_vec((bf16_t*)p.out + row_offset(p, b, kh, row, (long long)p.Lq * ld, ld) + at, o);
 }
 
-// Rows of segment 0 that the mask (and the length) leaves, side by side per head, and how many they are per batch item: the pipelined loop then has
-// whole tiles of keys, and none for what is masked (its own words and biases per tile cost it 20 us of 150 at 7200 queries, 5120 keys, 10 heads of
-// 64, with every key there).  A workgroup copies those of 64 rows of a head; it counts the ones before them itself.
+// Rows of segment 0 that the mask (and the length) leaves, side by side per head, with zeros behind their d values, and how many they are per batch
+// item: the pipelined loop then has whole tiles of keys, and none for what is masked (its own words and biases per tile cost it 20 us of 150 at 7200
+// queries, 5120 keys, 10 heads of 64, with every key there).  A workgroup copies those of 64 rows of a head; it counts the ones before them itself.
+// Bound by memory: 512 rows of 8 heads of 128 take 6 us (the launch is 3 of them).
 __global__ __launch_bounds__(256) void keep_rows(QParams p, int tiles, bf16_t* ko, bf16_t* vo, int* counts) {
   __shared__ int before[4];
   __shared__ unsigned long long word;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tile = (int)(blockIdx.x % tiles), bh = (int)(blockIdx.x / tiles), b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
   const int n = p.seg[0].n, n0 = seg0_rows(p, b);
-  const unsigned char* mask = p.mask + (long long)b * n;
+  const unsigned char* mask = p.mask ? p.mask + (long long)b * n : nullptr;
   const int row0 = tile * 64, upto = row0 < n0 ? row0 : n0;
   int mine = 0;
-  for (int i = tid * 16; i + 16 <= upto; i += 4096) {
-    unsigned int x[4];
-    __builtin_memcpy(x, mask + i, 16);
+  if (mask) {
+    for (int i = tid * 16; i + 16 <= upto; i += 4096) {
+      unsigned int x[4];
+      __builtin_memcpy(x, mask + i, 16);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) mine += __popc((((x[e] & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x[e]) & 0x80808080u);        // bytes that are not 0
+      for (int e = 0; e < 4; ++e) mine += __popc((((x[e] & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x[e]) & 0x80808080u);      // bytes that are not 0
+    }
+    if (tid < (upto & 15)) mine += mask[(upto & ~15) + tid] != 0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
   }
-  if (tid < (upto & 15)) mine += mask[(upto & ~15) + tid] != 0;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
   if (lane == 0) before[wave] = mine;
   if (wave == 0) {
-    const unsigned long long w = __builtin_amdgcn_ballot_w64(row0 + lane < n0 && mask[row0 + lane] != 0);
+    const unsigned long long w = __builtin_amdgcn_ballot_w64(row0 + lane < n0 && (!mask || mask[row0 + lane] != 0));
     if (lane == 0) word = w;
   }
   __syncthreads();
-  const int first = before[0] + before[1] + before[2] + before[3];
+  const int first = mask ? before[0] + before[1] + before[2] + before[3] : upto;
   const unsigned long long w = word;
   if (tile == tiles - 1 && kh == 0 && tid == 0) counts[b] = first + __popcll(w);
   const Seg& s = p.seg[0];
   const bf16_t* k = (const bf16_t*)s.k + (long long)b * s.bsk + (long long)kh * s.hsk;
   const bf16_t* v = (const bf16_t*)s.v + (long long)b * s.bsv + (long long)kh * s.hsv;
   const long long to0 = ((long long)b * p.kv_heads + kh) * n + first;
-  const int chunks = p.d / 8;
-  for (int i = tid; i < 64 * chunks; i += 256) {
-    const int r = i / chunks, at = (i - r * chunks) * 8;
+  const int D = p.d <= 64 ? 64 : 128;
+  for (int i = tid; i < 8 * D; i += 256) {
+    const int r = i / (D / 8), at = (i - r * (D / 8)) * 8;
     if (!((w >> r) & 1)) continue;
-    const long long to = (to0 + __popcll(w & low_bits(r))) * p.d + at;
-    *reinterpret_cast<u32x4*>(ko + to) = *reinterpret_cast<const u32x4*>(k + (row0 + r) * s.ldk + at);
-    *reinterpret_cast<u32x4*>(vo + to) = *reinterpret_cast<const u32x4*>(v + (row0 + r) * s.ldv + at);
+    const long long to = (to0 + __popcll(w & low_bits(r))) * D + at;
+    u32x4 a = {0u, 0u, 0u, 0u}, z = a;
+    if (at < p.d) {
+      a = *reinterpret_cast<const u32x4*>(k + (row0 + r) * s.ldk + at);
+      z = *reinterpret_cast<const u32x4*>(v + (row0 + r) * s.ldv + at);
+    }
+    *reinterpret_cast<u32x4*>(ko + to) = a;
+    *reinterpret_cast<u32x4*>(vo + to) = z;
   }
 }
 
@@ -825,6 +833,20 @@ __global__ __launch_bounds__(64 * NW, 2) void held_attn(QParams p, int row_group
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0070);                      // the wave's loads have landed
+  __syncthreads();
+  // Rows that are no keys, and what lies behind the d values of one, become zeros: a weight of 0 times what was read there need not be 0
+  for (int u = wave; u < 2 * nt; u += NW) {
+    const int i = u >> 1, isv = u & 1;
+    const unsigned long long bits = words[i];
+    if (bits == 0 || (bits == ~0ULL && p.d == D) || (KV4 && lo + i < tiles0)) continue;
+    char* const to = smem + (2 * i + isv) * TILE;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int r = j * RPI + lane / CH, at = lane % CH;
+      const int kc = (at ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 8;
+      if (!((bits >> r) & 1) || (!isv && kc >= p.d)) *reinterpret_cast<u32x4*>(to + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
   __syncthreads();
 
   for (; row0 < p.rows; row0 += step) {
@@ -1120,10 +1142,10 @@ __global__ __launch_bounds__(256) void float_attn(QParams p, int kw) {
         for (int db = 0; db < DB; ++db) v[db][e] = from[32 * db + c < p.d ? 32 * db + c : 0];
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (bits != 0xffffffffu) {
+      if (bits != 0xffffffffu || p.d != D) {
 #pragma unroll
         for (int j = 0; j < D / 8; ++j)
-          if (!valid) k[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (!valid || 8 * j + 4 * g >= p.d) k[j] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       scores(k);
       __builtin_amdgcn_sched_barrier(0);
@@ -1378,6 +1400,8 @@ struct Task {
   bool cached, masked, period;
 };
 
+constexpr long long kMostGroups = (1LL << 24) - 1;         // of 256 work items: a launch counts those in 32 bits
+
 // Microseconds of writing and merging `parts` rows of partial results
 double merge_us(double parts, int d) { return 3.3 + parts * (d + 2) * 8.0 / 3.5e6; }
 
@@ -1404,7 +1428,7 @@ double plan_held(const Task& k, long long ns, int nw, Plan& r) {
   const long long each = fit < 1 ? groups : (groups + fit - 1) / fit;      // blocks of a wave
   r.row_groups = (int)((groups + each - 1) / each);
   const long long wgs = r.row_groups * heads * r.nsplit, rounds = (wgs + 256 * cap - 1) / (256 * cap);
-  if (wgs > 0x7fffffffLL) return 1e30;
+  if (wgs > kMostGroups / 2) return 1e30;
   const long long on_cu = rounds > 1 ? cap : (wgs + 255) / 256;
   const bool two = on_cu * nw > 4;
   const double tile = D == 64 ? (two ? 1.2 : 0.7) : (two ? 2.1 : 1.15);
@@ -1423,7 +1447,10 @@ double plan_rows(const Task& k, int qb, Plan& r) {
   r.kind = kRows; r.nq = qb; r.block = 128 * qb; r.tile = 64;
   const long long tiles0 = (keys0 + 63) / 64 + (keys1 + 63) / 64, tiles = tiles0 > 0 ? tiles0 : 1;
   const long long blocks = heads * ((k.rows + r.block - 1) / r.block), all = blocks * tiles;
-  if (k.cached || k.masked) r.expand = ((size_t)heads * keys0 * k.d * 4 + 255) / 256 * 256 + (k.masked ? ((size_t)k.B * 4 + 255) / 256 * 256 : 0);
+  const int D = k.d <= 64 ? 64 : 128;
+  const bool copied = k.cached || k.masked || k.d != D;
+  if (copied) r.expand = ((size_t)heads * keys0 * D * 4 + 255) / 256 * 256 + (k.cached ? 0 : ((size_t)k.B * 4 + 255) / 256 * 256);
+  if (blocks > kMostGroups || (copied && (k.cached ? 1 : heads) * tiles > kMostGroups)) return 1e30;
   // Whole blocks, the same number each, where that takes hardly longer than cutting the line into as many equal shares as workgroups fit the chip
   // (the parts and their merge cost about as much as kCut tiles); shares of four tiles or more.
   constexpr long long kCut = 10;
@@ -1444,7 +1471,7 @@ double plan_rows(const Task& k, int qb, Plan& r) {
   const bool two = fit == 512 && s.count > 256;
   const double tile = k.d > 64 ? 1.1 : qb == 2 ? 1.1 : two ? 1.16 : 0.85;
   return (qb == 2 ? 12.0 : k.d > 64 ? 7.7 : 6.2) + tile * (double)(s.per + 1) * (double)((s.count + fit - 1) / fit) +
-         (r.parts ? merge_us(1.2 * (double)s.count * r.block, k.d) : 0.0) + (k.cached || k.masked ? 4.0 + (double)(heads * keys0) * k.d * (k.cached ? 4.5 : 8.0) / 4e6 : 0.0);
+         (r.parts ? merge_us(1.2 * (double)s.count * r.block, k.d) : 0.0) + (copied ? 4.0 + (double)(heads * keys0) * D * (k.cached ? 4.5 : 8.0) / 4e6 : 0.0);
 }
 
 // Full precision: `kw` waves of a workgroup on the same rows.  A tile of 32 keys takes a wave 1.55 us at 32 values, 2.6 at 64 and 4.6 at 128 (1200
@@ -1457,7 +1484,7 @@ double plan_float(const Task& k, int kw, long long ns, Plan& r) {
   r.tiles_per_split = (int)((tiles + ns - 1) / ns);
   r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
   const long long wgs = heads * ((k.rows + r.block - 1) / r.block) * r.nsplit, each = (r.tiles_per_split + kw - 1) / kw;
-  if (wgs > 0x7fffffffLL) return 1e30;
+  if (wgs > kMostGroups) return 1e30;
   if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * k.rows * (k.d + 2) * sizeof(float);
   const double tile = (0.5 + 1.03 * (k.d <= 32 ? 1 : k.d <= 64 ? 2 : 4)) * (wgs > 256 ? 1.15 : 1.0);
   return 4.5 + tile * (double)(((wgs + 255) / 256) * each) + (r.nsplit > 1 ? merge_us((double)r.nsplit * heads * k.rows, k.d) : 0.0);
@@ -1478,7 +1505,7 @@ double plan_few(const Task& k, Plan& r) {
   if (ns > 64) ns = 64;
   r.tiles_per_split = (int)((tiles + ns - 1) / ns);
   r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
-  if (blocks * r.nsplit > 0x7fffffffLL) return 1e30;
+  if (blocks * r.nsplit > kMostGroups) return 1e30;
   if (r.nsplit > 1) r.parts = (size_t)r.nsplit * heads * k.rows * (k.d + 2) * sizeof(float);
   return 6.0 + (k.d == 64 ? 1.05e-3 : 1.2e-3) * (double)(blocks * tiles) + (r.nsplit > 1 ? merge_us((double)r.nsplit * heads * k.rows, k.d) : 0.0);
 }
@@ -1507,8 +1534,8 @@ Plan choose(const Task& k) {
   }
   const char* form = tune_env("DF_QATTN");
   if (k.cached && own == 0 && (form ? !strcmp(form, "few") : rows <= 64)) {
-    plan_few(k, r);
-    return r;
+    r.ok = plan_few(k, q) < 1e29;
+    return r.ok ? q : r;
   }
   // The form that is predicted to take least
 #ifdef DF_TUNING
@@ -1615,14 +1642,14 @@ int launch_qattn(const QAttnArgs& a, hipStream_t st) {
   const long long nwg = r.kind == kRows ? r.share.count : r.kind == kHeld ? (long long)r.row_groups * a.kv_heads * a.B * r.nsplit : (rows + r.block - 1) / r.block * a.kv_heads * a.B * r.nsplit;
   if (nwg > 0x7fffffffLL) return DF_ESHAPE;
   const dim3 grid((unsigned)nwg);
-  if (r.expand && !cached && keys0 > 0) {                  // the rows that the mask leaves, and their number
-    bf16_t *k = (bf16_t*)a.workspace, *v = k + (size_t)a.B * a.kv_heads * keys0 * a.d;
-    int* const counts = (int*)((char*)a.workspace + ((size_t)a.B * a.kv_heads * keys0 * a.d * 4 + 255) / 256 * 256);
-    const int tiles = (int)((keys0 + 63) / 64);
+  if (r.expand && !cached) {                               // the rows that count, and their number
+    const int D = a.d <= 64 ? 64 : 128, tiles = (int)((keys0 + 63) / 64);
+    bf16_t *k = (bf16_t*)a.workspace, *v = k + (size_t)a.B * a.kv_heads * keys0 * D;
+    int* const counts = (int*)((char*)a.workspace + ((size_t)a.B * a.kv_heads * keys0 * D * 4 + 255) / 256 * 256);
     hipLaunchKernelGGL(keep_rows, dim3((unsigned)((long long)tiles * a.kv_heads * a.B)), dim3(256), 0, st, p, tiles, k, v, counts);
     DF_LAUNCH_CHECK();
     Seg& s = p.seg[0];
-    s.k = k; s.v = v; s.ldk = s.ldv = a.d; s.hsk = s.hsv = keys0 * a.d; s.bsk = s.bsv = keys0 * a.d * a.kv_heads;
+    s.k = k; s.v = v; s.ldk = s.ldv = D; s.hsk = s.hsv = keys0 * D; s.bsk = s.bsv = keys0 * D * a.kv_heads;
     p.lens = counts;
   }
   if (r.expand && cached) {

@@ -176,7 +176,7 @@ int launch_qk_norm_rope(const RopeArgs& a, hipStream_t st) {
   p.per_token = (unsigned int)cdiv(all, 4);
   p.steps = cdiv(all, p.per_token);
   const long long waves = (long long)a.B * a.T * p.per_token;
-  if (waves > 0x7fffffffLL) return DF_ESHAPE;
+  if (waves > (1LL << 26) - 4) return DF_ESHAPE;          // (a launch counts its work items in 32 bits)
   p.waves = (unsigned int)waves;
   p.per_token_recip = reciprocal_u32(p.per_token);
   p.T_recip = reciprocal_u32((unsigned int)a.T);

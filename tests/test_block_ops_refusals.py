@@ -42,7 +42,7 @@ def _rope(q=A, k=A, qo=A, ko=A, ld=256, bs=2048, old=256, obs=2048, qg=A, rot=A,
     (dict(qg=A + 4), EINVAL), (dict(rot=A + 8), EINVAL), (dict(pos=A + 2), EINVAL), (dict(old=0), EINVAL), (dict(obs=0), EINVAL),
     (dict(B=0), ESHAPE), (dict(T=0), ESHAPE), (dict(heads=0), ESHAPE), (dict(kv=0), ESHAPE), (dict(k=None, ko=None), ESHAPE), (dict(d=60), ESHAPE),
     (dict(d=264), ESHAPE), (dict(rot_dim=0), ESHAPE), (dict(rot_dim=12), ESHAPE), (dict(rot_dim=72), ESHAPE), (dict(rows=7), ESHAPE), (dict(rows=0), ESHAPE),
-    (dict(T=1 << 30, B=4, rows=1 << 30, obs=1 << 40), ESHAPE),
+    (dict(T=1 << 30, B=4, rows=1 << 30, obs=1 << 40), ESHAPE), (dict(T=1 << 26, B=1, rows=1 << 26), ESHAPE),
 ])
 def test_qk_norm_rope(kw, rc):
     assert _rope(**kw) == rc
@@ -56,7 +56,7 @@ def _refresh(c=A, k=A, v=A, ld=256, bs=2048, B=2, H=4, W=16, kv=4, d=64, patch=0
     (dict(c=None), EINVAL), (dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(c=A + 8), EINVAL), (dict(k=A + 8), EINVAL), (dict(ld=260), EINVAL),
     (dict(bs=-8), EINVAL), (dict(dt=3), EINVAL), (dict(axis=2), EINVAL), (dict(H=0), ESHAPE), (dict(N=0), ESHAPE), (dict(N=3), ESHAPE), (dict(patch=2), ESHAPE),
     (dict(patch=-1), ESHAPE), (dict(axis=1, N=3), ESHAPE), (dict(d=32), ESHAPE), (dict(B=0), ESHAPE), (dict(kv=0), ESHAPE), (dict(B=65536), ESHAPE),
-    (dict(H=1 << 16, W=1 << 15), ESHAPE),
+    (dict(H=1 << 16, W=1 << 15), ESHAPE), (dict(H=1 << 15, W=1 << 15), ESHAPE),
 ])
 def test_kv4_refresh(kw, rc):
     assert _refresh(**kw) == rc

@@ -133,3 +133,20 @@ def test_batch_items_with_different_numbers_of_keys(Lq, Lk, heads, kv, d, masked
     out = df.cross_attn(q, k, v, key_mask=mask.to(DEV) if masked else None, lens=torch.tensor(n, dtype=torch.int32, device=DEV) if lengths else None)
     assert out.isfinite().all()
     _check(out[:, rows], q[:, rows], host(k), host(v), True, valid)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("Lq,Lk,heads", [(5, 77, 2), (300, 1000, 2), (2000, 1500, 4)])
+def test_infinite_keys_of_no_weight_beside_padding(Lq, Lk, heads, bf16):
+    """d between the kernels' widths: a key whose scores are all -inf has weight 0, also where its infinities lie in the row's first values; and an
+    infinite value under a key does not become NaN by way of keys that are none."""
+    print("infinite", Lq, Lk, heads, bf16, flush=True)
+    d = 72 if bf16 else 40
+    q, k, v = _rows(1, 1, Lq, heads, d, bf16=bf16).abs() + 1, _rows(2, 1, Lk, heads, d, bf16=bf16), _rows(3, 1, Lk, heads, d, bf16=bf16)
+    w = k.clone()
+    w[:, 1::3, :, 2] = float("-inf")                         # (all queries are positive there)
+    valid = np.broadcast_to(np.arange(Lk)[None] % 3 != 1, (1, Lk))
+    rows = torch.tensor([0, 1, Lq // 2, Lq - 1])
+    got = df.cross_attn(q, w, v)
+    assert got.isfinite().all()
+    _check(got[:, rows], q[:, rows], host(k), host(v), bf16, valid)
