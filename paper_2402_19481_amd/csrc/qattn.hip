@@ -109,7 +109,7 @@ __device__ __forceinline__ Share share_of_keys(const QParams& p, Share s, int nr
 // slot, scalar ones too: runs of whole tiles of one segment go through a loop that only moves its pointers on.
 // Bound by instruction issue: of a tile's 1460 cycles (64 values; 215 instructions) the matrix unit works 512, and a second workgroup on the unit adds
 // 16 %.  7200 queries, 10 heads of 64: 5120 keys 124 us (0.76 PFLOP/s), 57600 rows of a cache 1150 (0.92); 16384 queries, 16 heads of 128 on 2048 keys
-// 300 us (0.92), on 512 keys 106 - 113 (8 tiles a block, whose beginning and end take the time of five).
+// 300 us (0.92), on 512 keys 104 - 110 (8 tiles a block, whose beginning and end take the time of five).
 // The running maximum is that of the first tile and moves when a row's weights of a tile sum to more than 2^13 (the sums are needed anyway; the
 // maximum of every tile would be 22 instructions more): by the power of two above the sum, which scales the packed weights exactly, or, beyond 2^100,
 // to the tile's own maximum, with the tile done again from its K in LDS.
@@ -603,23 +603,27 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
       const int at0 = wave * 32 * QB + 32 * n + c;
       bf16_t* op = (bf16_t*)p.out + row_offset(p, b, kh, row0 + 32 * n + c, (long long)p.Lq * p.kv_heads * p.group * p.d, (long long)p.kv_heads * p.group * p.d);
       float* po = p.part_o + ((long long)slot * BLK + at0) * p.d;
-      auto store = [&](int db, int f) DF_INLINE {
-        const int at = 32 * db + 16 * f + 8 * g;
-        float v[8];
+      auto store = [&](auto wholec, auto fullc) DF_INLINE {  // (branches outside: one pass of straight code)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = o[n][db][8 * f + e] * inv;
-        if (whole) {
-          st_vec(op + at, v);
-        } else {
-          st_vec(po + at, v);
-          st_vec(po + at + 4, v + 4);
-        }
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            const int at = 32 * db + 16 * f + 8 * g;
+            if (!decltype(fullc)::value && at >= p.d) continue;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = o[n][db][8 * f + e] * inv;
+            if (decltype(wholec)::value) {
+              st_vec(op + at, v);
+            } else {
+              st_vec(po + at, v);
+              st_vec(po + at + 4, v + 4);
+            }
+          }
       };
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-          if (p.d == D || 32 * db + 16 * f + 8 * g < p.d) store(db, f);
+      if (whole && p.d == D) store(std::true_type{}, std::true_type{});
+      else if (whole) store(std::true_type{}, std::false_type{});
+      else store(std::false_type{}, std::false_type{});
       if (!whole && g == 0) {
         float* ml = p.part_ml + 2 * ((long long)slot * BLK + at0);
         ml[0] = nt > 0 ? m[n] : -INFINITY;
