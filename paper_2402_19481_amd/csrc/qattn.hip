@@ -603,7 +603,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
       const int at0 = wave * 32 * QB + 32 * n + c;
       bf16_t* op = (bf16_t*)p.out + row_offset(p, b, kh, row0 + 32 * n + c, (long long)p.Lq * p.kv_heads * p.group * p.d, (long long)p.kv_heads * p.group * p.d);
       float* po = p.part_o + ((long long)slot * BLK + at0) * p.d;
-      auto store = [&](auto wholec, auto fullc) DF_INLINE {  // (branches outside: one pass of straight code)
+      auto store = [&](auto wholec, auto fullc) DF_INLINE {  // (branches outside: straight code; of 256 rows two forms, with three the loop has 16 moves more)
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -621,7 +621,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
             }
           }
       };
-      if (whole && p.d == D) store(std::true_type{}, std::true_type{});
+      if (QB == 1 && whole && p.d == D) store(std::true_type{}, std::true_type{});
       else if (whole) store(std::true_type{}, std::false_type{});
       else store(std::false_type{}, std::false_type{});
       if (!whole && g == 0) {
@@ -747,6 +747,7 @@ __global__ __launch_bounds__(256) void keep_rows(QParams p, int tiles, bf16_t* k
 // (pipelined 23).  KV4: segment 0 is the 4-bit cache itself, converted on its way to LDS (levels times scale is exact in bf16), V
 // transposed as it is held; the patch's own rows of it are no keys.
 constexpr int kHeldBytes = 128 * 1024;
+__device__ const u32x4 kZeros[1] = {};
 template <int D, int NW, bool MASK, bool KV4>
 __global__ __launch_bounds__(64 * NW, 2) void held_attn(QParams p, int row_groups, int own_tiles) {
   constexpr int TILE = 64 * D * 2, CH = D / 8, KS = D / 16, DB = D / 32, RPI = 1024 / (D * 2), NI = TILE / 1024;
@@ -800,13 +801,13 @@ __global__ __launch_bounds__(64 * NW, 2) void held_attn(QParams p, int row_group
       const Seg& s = p.seg[second ? 1 : 0];
       const long long ld = isv ? s.ldv : s.ldk;
       const bf16_t* src = (const bf16_t*)(isv ? s.v : s.k) + (long long)b * (isv ? s.bsv : s.bsk) + (long long)kh * (isv ? s.hsv : s.hsk) + (long long)t * 64 * ld;
-      const int some = __builtin_ctzll(bits);
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int r = j * RPI + lane / CH, at = lane % CH;
         const int kc = (at ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 8, vc = (at ^ (D == 64 ? ((r >> 1) & 1) * 2 ^ ((r >> 3) & 1) * 4 : (r & 3) * 4)) * 8;
-        const int ch = isv ? vc : kc, from = (bits >> r) & 1 ? r : some;
-        lds_load16(src + (long long)from * ld + (ch < p.d ? ch : 0), to + j * 1024);
+        const int ch = isv ? vc : kc;
+        const bool there = (bits >> r) & 1 && ch < p.d;    // else zeros: a weight of 0 times what else is read there need not be 0
+        lds_load16(there ? (const void*)(src + (long long)r * ld + ch) : (const void*)kZeros, to + j * 1024);
       }
     } else {
       const long long base = ((long long)b * p.kv_heads + kh) * p.c.pitch + (long long)t * 64;
@@ -841,20 +842,6 @@ __global__ __launch_bounds__(64 * NW, 2) void held_attn(QParams p, int row_group
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0070);                      // the wave's loads have landed
-  __syncthreads();
-  // Rows that are no keys, and what lies behind the d values of one, become zeros: a weight of 0 times what was read there need not be 0
-  for (int u = wave; u < 2 * nt; u += NW) {
-    const int i = u >> 1, isv = u & 1;
-    const unsigned long long bits = words[i];
-    if (bits == 0 || (bits == ~0ULL && p.d == D) || (KV4 && lo + i < tiles0)) continue;
-    char* const to = smem + (2 * i + isv) * TILE;
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int r = j * RPI + lane / CH, at = lane % CH;
-      const int kc = (at ^ (D == 64 ? (r >> 1) & 7 : r & 15)) * 8;
-      if (!((bits >> r) & 1) || (!isv && kc >= p.d)) *reinterpret_cast<u32x4*>(to + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
-    }
-  }
   __syncthreads();
 
   for (; row0 < p.rows; row0 += step) {
