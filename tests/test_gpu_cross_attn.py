@@ -114,7 +114,8 @@ def test_the_same_bits_and_a_given_result():
 
 
 @pytest.mark.parametrize("masked,lengths", [(True, False), (False, True), (True, True)])
-@pytest.mark.parametrize("Lq,Lk,heads,kv,d", [(2000, 1300, 8, 4, 64), (1500, 900, 8, 8, 128), (1111, 1027, 5, 5, 72), (6000, 4099, 4, 4, 64)])
+@pytest.mark.parametrize("Lq,Lk,heads,kv,d", [(2000, 1300, 8, 4, 64), (1500, 900, 8, 8, 128), (1111, 1027, 5, 5, 72), (6000, 4099, 4, 4, 64),
+                                              (6144, 6100, 4, 4, 64)])
 def test_batch_items_with_different_numbers_of_keys(Lq, Lk, heads, kv, d, masked, lengths):
     """Long enough for the pipelined form: the work is shared by the keys there are; what is no key holds NaN."""
     print("numbers", Lq, Lk, heads, kv, d, masked, lengths, flush=True)
@@ -150,3 +151,18 @@ def test_infinite_keys_of_no_weight_beside_padding(Lq, Lk, heads, bf16):
     got = df.cross_attn(q, w, v)
     assert got.isfinite().all()
     _check(got[:, rows], q[:, rows], host(k), host(v), bf16, valid)
+
+
+@pytest.mark.parametrize("Lq,bf16,masked", [(5, True, False), (2000, True, False), (2000, True, True), (300, False, False)])
+def test_offsets_beyond_32_bits(Lq, bf16, masked):
+    """Keys and values 2^20 values apart, 3000 of them."""
+    print("far", Lq, bf16, masked, flush=True)
+    Lk, heads, d = 3000, 2, 64
+    wide = torch.empty(Lk, 1 << 20, dtype=TYPES[bf16], device=DEV)
+    k, v = (wide[None, :, i * heads * d:(i + 1) * heads * d].unflatten(-1, (heads, d)) for i in range(2))
+    k.copy_(_rows(2, 1, Lk, heads, d, bf16=bf16)), v.copy_(_rows(3, 1, Lk, heads, d, bf16=bf16))
+    q = _rows(1, 1, Lq, heads, d, bf16=bf16)
+    valid = np.arange(Lk)[None] % 5 != 0 if masked else None
+    out = df.cross_attn(q, k, v, key_mask=torch.from_numpy(valid).to(DEV) if masked else None)
+    rows = torch.tensor([0, 1, Lq // 2, Lq - 1])
+    _check(out[:, rows], q[:, rows], host(k), host(v), bf16, valid)

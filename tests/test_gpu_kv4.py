@@ -78,6 +78,7 @@ def _check(got, q, k, v, bf16, valid=None, scale=None):
 @pytest.mark.parametrize("B,Lq,L,heads,kv,d", [
     (1, 1, 1, 1, 1, 64), (1, 1, 64, 2, 2, 64), (2, 1, 777, 8, 2, 64), (1, 3, 130, 4, 4, 128), (1, 16, 1000, 2, 2, 64), (2, 5, 333, 12, 3, 128),
     (1, 33, 65, 2, 1, 64), (1, 64, 260, 1, 1, 64), (1, 65, 200, 2, 2, 64), (2, 100, 511, 4, 2, 128), (1, 300, 70, 3, 3, 64), (1, 1, 9000, 1, 1, 64),
+    (2, 200, 900, 8, 4, 64), (2, 1300, 1600, 4, 4, 64), (1, 700, 1500, 8, 4, 128),
 ])
 def test_cached_attention(B, Lq, L, heads, kv, d, bf16):
     print("attn_kv4", B, Lq, L, heads, kv, d, bf16, flush=True)
@@ -102,6 +103,7 @@ def test_cached_attention(B, Lq, L, heads, kv, d, bf16):
 @pytest.mark.parametrize("B,H,W,N,cols,heads,kv,d", [
     (1, 1, 64, 1, False, 2, 2, 64), (1, 4, 30, 2, False, 2, 2, 64), (2, 6, 50, 3, False, 4, 2, 64), (1, 8, 40, 8, False, 3, 3, 128), (1, 7, 36, 4, True, 2, 2, 64),
     (2, 10, 33, 3, True, 2, 1, 128), (1, 1, 16, 16, False, 2, 2, 64), (1, 20, 60, 2, True, 1, 1, 64),
+    (1, 30, 100, 2, False, 4, 4, 64), (1, 30, 100, 2, True, 6, 3, 128), (2, 25, 90, 2, True, 4, 4, 64),
 ])
 def test_displaced_attention(B, H, W, N, cols, heads, kv, d, bf16):
     print("displaced kv4", B, H, W, N, cols, heads, kv, d, bf16, flush=True)
@@ -119,3 +121,23 @@ def test_displaced_attention(B, H, W, N, cols, heads, kv, d, bf16):
     else:
         got = df.attn_displaced_kv4(q, fk, fv, cache, patch, N)
     _check(got, q, hk, hv, bf16)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_a_cache_beyond_32_bits(bf16):
+    """64 heads of 2^20 rows, 4.5 GB: the last 1000 rows of the last heads, among zeros."""
+    L, h, d, n = 1 << 20, 64, 64, 1 << 10
+    cache = df.kv4_cache(1, L, h, d)
+    assert cache.numel() * cache.element_size() > 1 << 32
+    k, v, q = _rows(1, 1, n, h, d, bf16=bf16, std=3.0), _rows(2, 1, n, h, d, bf16=bf16), _rows(3, 1, 2, h, d, bf16=bf16, std=3.0)
+    df.kv4_refresh(cache, k, v, L // n - 1, L // n)
+    got = host(df.attn_kv4(q, cache, L, h))[:, :, -2:]
+    hk, hv = bo.held_in_4_bits(host(k))[:, :, -2:], bo.held_in_4_bits(host(v))[:, :, -2:]
+    hq = host(q)[:, :, -2:]
+    s = np.einsum("bqhd,bkhd->bhqk", hq, hk) * d ** -0.5
+    w = np.exp(s)
+    whole = w.sum(-1) + (L - n)                              # the zero rows have weight e^0 each
+    ref = np.einsum("bhqk,bkhd->bqhd", w / whole[..., None], hv)
+    size = np.einsum("bhqk,bkhd->bqhd", w / whole[..., None], np.abs(hv))
+    reach = np.abs(np.einsum("bqhd,bkhd->bhqk", np.abs(hq), np.abs(hk))).max() * d ** -0.5
+    assert (np.abs(got - ref) <= bo.attention_bound(ref, size, reach, d, L, bf16)).all() and np.abs(got).max() > 0
