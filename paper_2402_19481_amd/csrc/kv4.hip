@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Params p) {
 }
 
 // The rows that are not the patch's as bf16, side by side per head: what attention with many queries reads (qattn.hip), the conversion
-// once for all blocks of rows.  8400 rows of 10 heads of 64: 7.0 us, 50400: 25.7 (4 TB/s)
+// once for all blocks of rows.  8400 rows of 10 heads of 64: 7.0 us, 50400: 25.7 (168 MB, 6.5 TB/s)
 template <int D>
 __global__ __launch_bounds__(256) void kv4_expand_kernel(Kv4Params p, const int* lens, long long rows) {
   constexpr int G = D / 8, ROWS = 256 / G, PASS = 64 / ROWS, PITCH = G + 1;

@@ -266,15 +266,6 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
     const int lo = blk.lo, n0 = blk.n0, n1 = p.seg[1].n, tiles0 = blk.tiles0, b = blk.b, kh = blk.kh, row0 = blk.row0;
     const bool whole = blk.whole, idle = row0 >= p.rows;
     const unsigned int slot = 2 * w + (lo == 0 ? 1 : 0);
-#pragma unroll
-    for (int n = 0; n < QB; ++n)
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        qreg[n][s] = qnext[n][s];
-        asm volatile("" : "+v"(qreg[n][s]));               // Q has arrived: the loop does not wait for it, with the direct loads
-        if (p.d != D && 16 * s + 8 * g >= p.d) qreg[n][s] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-      }
-
     f32x16 o[QB][DB], sa[QB][2];
     u32x4 pk[QB][4];
     float m[QB], l[QB];
@@ -511,6 +502,14 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
         for (int j = 0; j < LPT; ++j) load(va, vofs, j, VR + wofs);
         sync_tile();
       }
+#pragma unroll
+      for (int n = 0; n < QB; ++n)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          qreg[n][s] = qnext[n][s];
+          asm volatile("" : "+v"(qreg[n][s]));             // Q has arrived: the loop does not wait for it, with the direct loads
+          if (p.d != D && 16 * s + 8 * g >= p.d) qreg[n][s] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+        }
       // an iteration's loads, and at the last one the next block's Q
       auto begin = [&](int t) DF_INLINE {
         take();
