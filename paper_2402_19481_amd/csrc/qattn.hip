@@ -128,6 +128,7 @@ __global__ __launch_bounds__(256, D == 64 && QB == 1 ? 2 : 1) void rows_attn(QPa
   }
   unsigned int pos = share_begin(sh, w);
   const unsigned int end = share_begin(sh, w + 1);
+  if (pos >= end) return;                                  // fewer tiles than shares were planned: no block, and no batch item, is its
   // Direct load j of the wave covers tile rows (LPT wave + j) * RPI + lane / CH; the chunks of a row are swizzled by it.  (K and V have D
   // values a row; where d is less they are zeros, Q is too, those of O are dropped.)
   unsigned int kch[LPT], vch[LPT];

@@ -166,3 +166,25 @@ def test_offsets_beyond_32_bits(Lq, bf16, masked):
     out = df.cross_attn(q, k, v, key_mask=torch.from_numpy(valid).to(DEV) if masked else None)
     rows = torch.tensor([0, 1, Lq // 2, Lq - 1])
     _check(out[:, rows], q[:, rows], host(k), host(v), bf16, valid)
+
+
+@pytest.mark.parametrize("masked", [True, False])
+@pytest.mark.parametrize("d", [64, 72, 128])
+def test_hardly_any_keys_where_many_were_planned(d, masked):
+    """Workgroups for 4000 keys, of which a batch item has one or none: most of them are left without work."""
+    print("hardly any", d, masked, flush=True)
+    B, Lq, Lk, heads = 2, 2000, 4000, 2
+    q, k, v = _rows(1, B, Lq, heads, d), _rows(2, B, Lk, heads, d), _rows(3, B, Lk, heads, d)
+    for n in ([0, 0], [0, 1], [1, 0], [65, 1]):
+        valid = torch.arange(Lk)[None] < torch.tensor(n)[:, None]
+        if masked:
+            valid = valid.flip(1)
+            got = df.cross_attn(q, k, v, key_mask=valid.to(DEV))
+        else:
+            got = df.cross_attn(q, k, v, lens=torch.tensor(n, dtype=torch.int32, device=DEV))
+        rows = torch.tensor([0, 127, 128, Lq - 1])
+        _check(got[:, rows], q[:, rows], host(k), host(v), True, valid.numpy())
+        for b in range(B):
+            if n[b] < 2:                                     # one key: its values; none: zeros
+                at = Lk - 1 if masked else 0
+                assert torch.equal(got[b], v[b, at].expand(Lq, heads, d) if n[b] else torch.zeros_like(got[b]))
