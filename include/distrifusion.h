@@ -259,7 +259,7 @@ int df_cross_attn_packed(const void* xp, const void* wq_packed, const float* ln_
  *     Pair i of the first rot_dim values of a head is (2 i, 2 i + 1) if interleaved, else (i, i + rot_dim / 2):
  *     (a, b) -> (a cos - b sin, b cos + a sin).
  * d % 8 == 0, d <= 256; rot_dim % 8 == 0.  Addresses and strides: multiples of 16 bytes (float), 8 bytes (bf16; fastest with 16); gamma and rot
- * 16-byte aligned.  Sums are float: a row of values above 1e19 gives NaN.  B * T * ceil((heads + kv_heads) * lanes / 256) is at most 2^26 - 4, lanes =
+ * 16-byte aligned.  eps >= 0 and finite; with 0 a row of zeros gives NaN, as one with an infinity or NaN does, all of it.  B * T * ceil((heads + kv_heads) * lanes / 256) is at most 2^26 - 4, lanes =
  * d / 8 (float, or bf16 in multiples of 8 bytes: d / 4) rounded up to a power of two, 2 at least.
  */
 int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, void* q_out,

@@ -125,7 +125,22 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p) {
       float sq = 0.f;
 #pragma unroll
       for (int i = 0; i < V; ++i) sq = fmaf(x[u][i], x[u][i], sq);
-      const float v = fmaf(group_sum<G>(sq), p.inv_d, p.eps);
+      float v = fmaf(group_sum<G>(sq), p.inv_d, p.eps);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(v >= 0x1p-96f && v < INFINITY)) != 0, 0)) {
+        // Squares that left float's range, or are about to (what a square loses below 2^-126 is nothing beside 2^-96): the sum is that of the values
+        // times a power of two, f.  1 / sqrt(v) is then too small by f, which the values of a small row take on, and those of a large one, in halves
+        // with their scales, give up.
+        const float f = v < 0x1p-96f ? 0x1p100f : v < INFINITY ? 1.f : 0x1p-100f, half = f < 1.f ? 0x1p-50f : 1.f;
+        sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float y = x[u][i] * f;
+          sq = fmaf(y, y, sq);
+          x[u][i] = f > 1.f ? y : x[u][i] * half;
+          gx[u][i] *= half;
+        }
+        v = fmaf(group_sum<G>(sq), p.inv_d, p.eps * f * f);
+      }
       float r = __builtin_amdgcn_rsqf(v);
       r = fmaf(0.5f * r, fmaf(-v * r, r, 1.f), r);         // (the instruction is off by one unit in the last place)
 #pragma unroll
