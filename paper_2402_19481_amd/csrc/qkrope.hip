@@ -65,14 +65,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p) {
   const long long t = tok - b * (unsigned int)p.T;
   const bool in = e0 < p.d;
   const int n = 2 * p.half;
-  const bool turns = e0 < n;
+  const int at = p.pos ? p.pos[tok] : (int)t;
+  const bool turns = e0 < n && at >= 0;                    // (a token that does not turn keeps its values whatever their partners are)
 
   // angles of this lane's values, sign of the partner's share included: y = y * c + partner * s
   float c[V], s[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
-  const int at = p.pos ? p.pos[tok] : (int)t;
-  if (p.rot && turns && at >= 0) {
+  if (p.rot && turns) {
     if (at >= p.rot_len) {                                 // no such angles: the result must not pass for one
 #pragma unroll
       for (int i = 0; i < V; ++i) c[i] = __uint_as_float(0x7fc00000u);

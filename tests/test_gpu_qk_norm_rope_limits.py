@@ -1,4 +1,4 @@
-"""Norm of queries and keys at the ends of float's range.  Tolerances as in test_gpu_qk_norm_rope.py."""
+"""Norm and rotation at the ends of float's range, and of tokens that are not rotated.  Tolerances as in test_gpu_qk_norm_rope.py."""
 import numpy as np
 import pytest
 import torch
@@ -60,3 +60,22 @@ def test_rows_of_denormal_numbers_and_of_zeros(bf16):
     assert torch.equal(got[0, 0], torch.ones_like(got[0, 0])) and got[0, 1, 0, 5] == -8 and got[0, 1, 0].count_nonzero() == 1
     assert got[0, 1, 1].isnan().all() and got[0, 2].isnan().all()                    # 0 / 0
     assert not df.qk_norm_rope(x, eps=1e-6)[0][0, 2].any()
+
+
+@pytest.mark.parametrize("inter", [True, False])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_a_token_that_is_not_rotated_keeps_its_bits(bf16, inter):
+    """A negative position: no value depends on its partner, be that infinite or no number; zeros keep their sign."""
+    d, rot = 64, 32
+    x = torch.randn(1, 4, 3, d, generator=torch.Generator().manual_seed(2)).to(TYPES[bf16]).to(DEV)
+    x[..., 3], x[..., 20], x[..., 6] = float("inf"), float("nan"), -0.0
+    a = np.random.default_rng(1).uniform(0, 6, (2, rot // 2))
+    table = torch.from_numpy(np.stack((np.cos(a), np.sin(a)), -1).astype(np.float32)).to(DEV)
+    pos = torch.tensor([[-1, 1, -7, 2]], dtype=torch.int32, device=DEV)
+    got, _ = df.qk_norm_rope(x, rot=table, pos=pos, norm=False, interleaved=inter)
+    bits = torch.int16 if bf16 else torch.int32
+    for t in (0, 2):
+        number = ~x[0, t].isnan()                            # (what a NaN's bits are is nobody's promise)
+        assert torch.equal(got[0, t].view(bits)[number], x[0, t].view(bits)[number]) and got[0, t][~number].isnan().all()
+    assert got[0, 3, :, :rot].isnan().all() and not torch.equal(got[0, 1, :, :rot], x[0, 1, :, :rot])
+    assert torch.equal(got[0, 3, :, rot:], x[0, 3, :, rot:])
