@@ -272,7 +272,7 @@ int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k
  * 64 values).  Each row (token, head) of d values is held as the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times a scale (of two equally near
  * ones 0, 1, 2 or 4), with sign; the scale is a sixth of the row's largest magnitude, rounded to six significant bits, so that what is held is
  * exact in bf16.  A row with an infinity or NaN is NaN as a whole, one below 2^-100 is zero.
- *   cache  device memory of df_kv4_bytes(B, L, kv_heads, d), 16-byte aligned, d 64 or 128, L < 2^30 - 63 (0 for sizes it does not take); rows must be
+ *   cache  device memory of df_kv4_bytes(B, L, kv_heads, d), 16-byte aligned, d 64 or 128, L < 2^30 - 63, at most 2^40 rows of all heads (0 for sizes it does not take); rows must be
  *          written before they are read, zeroed memory holds zeros.
  *   df_kv4_refresh  the rows of patch `patch_idx` of N of an H x W grid of tokens (L = H * W; split as in the *_axis functions) receive
  *          k, v [B, L / N, kv_heads, d], strides as above (16-byte multiples); one token of a sequence is patch t of N = L.  Other rows keep

@@ -334,9 +334,10 @@ int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k
   return launch_qk_norm_rope(a, (hipStream_t)stream);
 }
 
-// Sizes of a 4-bit cache that the kernels take
+// Sizes of a 4-bit cache that the kernels take (launches: 32 bits of work items; all rows' bytes: 64)
 static inline bool kv4_sizes(long long B, long long L, int kv_heads, int d) {
-  return B > 0 && L > 0 && kv_heads > 0 && B <= 65535 && kv_heads <= 65535 && L <= (1LL << 30) - 64 && (d == 64 || d == 128);   // (launches: 32 bits of work items)
+  return B > 0 && L > 0 && kv_heads > 0 && B <= 65535 && kv_heads <= 65535 && L <= (1LL << 30) - 64 && (d == 64 || d == 128) &&
+         B * kv_heads * kv4_pitch(L) <= 1LL << 40;
 }
 
 size_t df_kv4_bytes(int B, int L, int kv_heads, int d) { return kv4_sizes(B, L, kv_heads, d) ? kv4_bytes(B, L, kv_heads, d) : 0; }
