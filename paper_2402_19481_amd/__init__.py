@@ -307,11 +307,14 @@ def qk_norm_rope(q, k=None, q_gamma=None, k_gamma=None, rot=None, pos=None, eps=
 
 
 def kv4_cache(B, L, kv_heads, d, device="cuda"):
-    """An empty 4-bit cache of L rows of keys and values (all zero; see the header for what a row holds)."""
+    """An empty 4-bit cache of L rows of keys and values (all zero; see the header for what a row holds and how).
+
+    Its shape [d + 4, B, kv_heads, L rounded up to 64] tells its sizes, which the calls check; it has no meaning per element.  Flat memory of as
+    many bytes is taken too."""
     n = lib().df_kv4_bytes(B, L, kv_heads, d)
     if n == 0:
         raise DfError(f"no 4-bit cache of B={B}, L={L}, kv_heads={kv_heads}, d={d}")
-    return torch.zeros(n, dtype=torch.uint8, device=device)
+    return torch.zeros(d + 4, B, kv_heads, n // ((d + 4) * B * kv_heads), dtype=torch.uint8, device=device)
 
 
 def kv4_refresh(cache, k, v, patch_idx, N):

@@ -188,13 +188,16 @@ void* given(PyObject* o, at::ScalarType type, std::initializer_list<int64_t> siz
 void together(const at::Tensor& a, PyObject* o) {
   if (o != Py_None && tensor(o).device() != a.device()) fail(g_error, "tensors must be on the same GPU");
 }
-// A 4-bit cache of these sizes
+// A 4-bit cache of these sizes.  kv4_cache makes it [d + 4, B, kv_heads, rows], so that sizes of as many bytes are told apart (and a slice along
+// any of them is not contiguous or has other sizes); memory of a caller's own in another form goes by its bytes.
 void* cache_of(PyObject* o, const at::Tensor& like, int B, long long L, int kv_heads, int d) {
   const at::Tensor& t = tensor(o);
   if (t.scalar_type() != at::kByte || !t.is_contiguous() || !t.is_cuda() || t.device() != like.device())
     fail(g_error, "cache: expected a tensor of kv4_cache on the same GPU");
   const size_t bytes = L > 0x7fffffffLL ? 0 : g_kv4_bytes(B, (int)L, kv_heads, d);
-  if (bytes == 0 || (size_t)t.numel() != bytes) fail(PyExc_ValueError, "cache: not one of these sizes");
+  const bool made = t.dim() == 4;
+  if (bytes == 0 || (size_t)t.numel() != bytes || (made && (t.size(0) != d + 4 || t.size(1) != B || t.size(2) != kv_heads)))
+    fail(PyExc_ValueError, "cache: not one of these sizes");
   return t.data_ptr();
 }
 at::Tensor result(const at::Tensor& q, PyObject* out, bool& made) {
