@@ -19,6 +19,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 SOURCE_FLAGS = {"qattn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
+def flags(src):
+    """What the library compiles a source with."""
+    return [*FLAGS, *SOURCE_FLAGS.get(src, [])]
+
+
 # The tuning build (python -m paper_2402_19481_amd.build --tuning) compiles the environment switches in (DF_TG,
 # DF_TGS, DF_ATTN_SPLITS, ...: kernel-selection overrides for sweeps such as `bench.py --tile-sweep`) and writes
 # libdistrifusion_tune.so beside the library; the library proper never reads the environment.
@@ -48,7 +53,7 @@ def _compile_binding():
 
 def _compile(src, tuning=False):
     obj = os.path.join(OBJ_TUNE if tuning else OBJ, src.replace(".hip", ".o"))
-    cmd = ["hipcc", *FLAGS, *SOURCE_FLAGS.get(src, []), *(["-DDF_TUNING"] if tuning else []), "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = ["hipcc", *flags(src), *(["-DDF_TUNING"] if tuning else []), "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:
