@@ -1381,7 +1381,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kv4(QParams p) {
 enum { kRows, kHeld, kFewKv4, kFloat };
 struct Plan {
   int kind, nq;                                // nq: blocks of 16 (kFewKv4) or of 32 rows a wave (kRows), waves (kHeld), waves on the same rows (kFloat)
-  int block, tile;                             // rows of a workgroup, keys of a tile
+  int block;                                   // rows of a workgroup
   int nsplit, tiles_per_split;                 // all but kRows
   int row_groups, own_tiles;                   // kHeld
   Share share;                                 // kRows
@@ -1408,7 +1408,7 @@ double plan_held(const Task& k, long long ns, int nw, Plan& r) {
   r.ok = true;
   const long long heads = (long long)k.B * k.kv_heads;
   const int D = k.d <= 64 ? 64 : 128, held = 2 * 64 * D * 2, most = kHeldBytes / held;
-  r.kind = kHeld; r.tile = 64;
+  r.kind = kHeld;
   if (k.cached && k.own > 0 && !k.period) {
     const long long first = (k.own_lo + 63) / 64, last = (k.own_lo + k.own) / 64;
     if (last > first) r.own_tiles = (int)(last - first);
@@ -1440,7 +1440,7 @@ double plan_rows(const Task& k, int qb, Plan& r) {
   r = Plan{};
   r.ok = true;
   const long long heads = (long long)k.B * k.kv_heads, keys0 = k.cached ? k.L - k.own : k.L, keys1 = k.cached ? k.own : 0;
-  r.kind = kRows; r.nq = qb; r.block = 128 * qb; r.tile = 64;
+  r.kind = kRows; r.nq = qb; r.block = 128 * qb;
   const long long tiles0 = (keys0 + 63) / 64 + (keys1 + 63) / 64, tiles = tiles0 > 0 ? tiles0 : 1;
   const long long blocks = heads * ((k.rows + r.block - 1) / r.block), all = blocks * tiles;
   const int D = k.d <= 64 ? 64 : 128;
@@ -1476,7 +1476,7 @@ double plan_float(const Task& k, int kw, long long ns, Plan& r) {
   r = Plan{};
   r.ok = true;
   const long long heads = (long long)k.B * k.kv_heads, own = k.cached ? k.own : 0, tiles = (k.L + 31) / 32 + (own + 31) / 32;
-  r.kind = kFloat; r.nq = kw; r.block = 128 / kw; r.tile = 32;
+  r.kind = kFloat; r.nq = kw; r.block = 128 / kw;
   r.tiles_per_split = (int)((tiles + ns - 1) / ns);
   r.nsplit = (int)((tiles + r.tiles_per_split - 1) / r.tiles_per_split);
   const long long wgs = heads * ((k.rows + r.block - 1) / r.block) * r.nsplit, each = (r.tiles_per_split + kw - 1) / kw;
@@ -1492,7 +1492,7 @@ double plan_few(const Task& k, Plan& r) {
   r = Plan{};
   r.ok = true;
   const long long heads = (long long)k.B * k.kv_heads, tiles = (k.L + 63) / 64;
-  r.kind = kFewKv4; r.nq = k.rows > 16 ? 2 : 1; r.block = 16 * r.nq; r.tile = 64;
+  r.kind = kFewKv4; r.nq = k.rows > 16 ? 2 : 1; r.block = 16 * r.nq;
   const long long blocks = heads * ((k.rows + r.block - 1) / r.block);
   long long ns = 1;
   if (blocks < 768) ns = 768 / blocks;
