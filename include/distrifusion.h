@@ -287,7 +287,7 @@ int df_kv4_read(const void* cache, void* k, void* v, int B, int L, int kv_heads,
 /*
  * Attention over a 4-bit cache, and to an encoder's states.  out [B, Lq, heads, d] (contiguous) = softmax(q k^T * scale) v per head; heads
  * is a multiple of kv_heads, and heads h of a group share key head h / (heads / kv_heads).  q and other rows: strides as above, in multiples of
- * 16 bytes, rows of k and v at most 2^24 elements apart.  scale positive and finite.  A query without any key gives zeros.  bf16 rounds the weights of the keys to bf16 for the matrix
+ * 16 bytes, rows of k and v at most 2^24 elements apart.  scale positive and below 2.35e38.  A query without any key gives zeros.  bf16 rounds the weights of the keys to bf16 for the matrix
  * instructions; everything else is float.
  *   df_attn_kv4            all keys from the cache: its L rows, or the first lens[b] of batch item b (device memory, NULL: L; clamped to
  *                          0 .. L; what the other rows hold does not matter).

@@ -388,6 +388,7 @@ static inline int qattn_sizes(int B, int Lq, long long L, int heads, int kv_head
 }
 // Rows of keys and values: the kernels' offsets within a tile of them are 32 bits
 static inline bool far_rows(long long rows, long long k_ld, long long v_ld) { return rows > 1 && (k_ld > (1LL << 24) || v_ld > (1LL << 24)); }
+static inline bool bad_scale(float scale) { return !(scale > 0.f && scale * 1.4426950408889634f < INFINITY); }   // (the kernels' exponentials are of base 2)
 static inline bool bad_workspace(const void* w) { return (uintptr_t)w % 256 != 0; }
 
 size_t df_cross_attn_workspace_bytes(int B, int Lq, int Lk, int heads, int kv_heads, int d, int masked, int dtype) {
@@ -398,7 +399,7 @@ size_t df_cross_attn_workspace_bytes(int B, int Lq, int Lk, int heads, int kv_he
 int df_cross_attn(const void* q, long long q_ld, long long q_bs, const void* k, long long k_ld, long long k_bs, const void* v, long long v_ld,
                   long long v_bs, const unsigned char* key_mask, const int* lens, void* out, int B, int Lq, int Lk, int heads, int kv_heads,
                   int d, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!q || !k || !v || !out || bad_dtype(dtype) || !(scale > 0.f && scale < INFINITY)) return DF_EINVAL;
+  if (!q || !k || !v || !out || bad_dtype(dtype) || bad_scale(scale)) return DF_EINVAL;
   if (bad_rows(q, q_ld, q_bs, dtype) || bad_rows(k, k_ld, k_bs, dtype) || bad_rows(v, v_ld, v_bs, dtype)) return DF_EINVAL;
   if ((uintptr_t)out % 16 || (uintptr_t)lens % 4 || bad_workspace(workspace)) return DF_EINVAL;
   const int rc = qattn_sizes(B, Lq, Lk, heads, kv_heads, d);
@@ -419,7 +420,7 @@ size_t df_attn_kv4_workspace_bytes(int B, int Lq, int L, int heads, int kv_heads
 
 int df_attn_kv4(const void* q, long long q_ld, long long q_bs, const void* cache, const int* lens, void* out, int B, int Lq, int L, int heads,
                 int kv_heads, int d, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!q || !cache || !out || bad_dtype(dtype) || !(scale > 0.f && scale < INFINITY) || bad_rows(q, q_ld, q_bs, dtype)) return DF_EINVAL;
+  if (!q || !cache || !out || bad_dtype(dtype) || bad_scale(scale) || bad_rows(q, q_ld, q_bs, dtype)) return DF_EINVAL;
   if (((uintptr_t)out | (uintptr_t)cache) % 16 || (uintptr_t)lens % 4 || bad_workspace(workspace)) return DF_EINVAL;
   if (!kv4_sizes(B, L, kv_heads, d)) return DF_ESHAPE;
   const int rc = qattn_sizes(B, Lq, L, heads, kv_heads, d);
@@ -442,7 +443,7 @@ size_t df_attn_displaced_kv4_workspace_bytes(int B, int H, int W, int heads, int
 int df_attn_displaced_kv4(const void* q, long long q_ld, long long q_bs, const void* k_fresh, long long k_ld, long long k_bs, const void* v_fresh,
                           long long v_ld, long long v_bs, const void* cache, void* out, int B, int H, int W, int heads, int kv_heads, int d,
                           int patch_idx, int N, float scale, int dtype, int split_axis, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!q || !k_fresh || !v_fresh || !cache || !out || bad_dtype(dtype) || !(scale > 0.f && scale < INFINITY)) return DF_EINVAL;
+  if (!q || !k_fresh || !v_fresh || !cache || !out || bad_dtype(dtype) || bad_scale(scale)) return DF_EINVAL;
   if (bad_rows(q, q_ld, q_bs, dtype) || bad_rows(k_fresh, k_ld, k_bs, dtype) || bad_rows(v_fresh, v_ld, v_bs, dtype)) return DF_EINVAL;
   if (((uintptr_t)out | (uintptr_t)cache) % 16 || bad_workspace(workspace)) return DF_EINVAL;
   QAttnArgs a = {};
