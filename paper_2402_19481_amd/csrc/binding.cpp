@@ -401,6 +401,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t na) {
     if (a[1] != Py_None) {
       hk = heads(a[1], "k");
       same(hq, hk, true, false, "k: expected [B, T, kv_heads, d] like q");
+      if (hk.H == 0) fail(PyExc_ValueError, "k: no heads");
       together(q, a[1]);
     } else if (a[10] != Py_None) {
       fail(PyExc_ValueError, "k_out without k");
