@@ -272,10 +272,11 @@ int df_qk_norm_rope(const void* q, long long q_ld, long long q_bs, const void* k
  * 64 values).  Each row (token, head) of d values is held as the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times a scale (of two equally near
  * ones 0, 1, 2 or 4), with sign; the scale is a sixth of the row's largest magnitude, rounded to six significant bits, so that what is held is
  * exact in bf16.  A row with an infinity or NaN is NaN as a whole, one below 2^-100 is zero.
- *   cache  device memory of df_kv4_bytes(B, L, kv_heads, d), 16-byte aligned, d 64 or 128, L < 2^30 - 63, at most 2^40 rows of all heads (0 for sizes it does not take); rows must be
- *          written before they are read, zeroed memory holds zeros.
+ *   cache  device memory of df_kv4_bytes(B, L, kv_heads, d), 16-byte aligned, d 64 or 128, L < 2^30 - 63, at most 2^40 rows of all heads (0 for
+ *          sizes it does not take); rows must be written before they are read, zeroed memory holds zeros.
  *   df_kv4_refresh  the rows of patch `patch_idx` of N of an H x W grid of tokens (L = H * W; split as in the *_axis functions) receive
- *          k, v [B, L / N, kv_heads, d], strides as above (16-byte multiples); one token of a sequence is patch t of N = L.  Other rows keep
+ *          k, v [B, L / N, kv_heads, d], strides as above (16-byte multiples); one token of a sequence is patch t of N = L.  Every batch
+ *          item's rows are the same ones: items of different lengths that grow by a token each need a cache each.  Other rows keep
  *          what they hold.  Two neighbouring tokens share bytes: refreshes of one cache must not overlap in time.
  *   df_kv4_read     k, v [B, L, kv_heads, d], contiguous: what all rows stand for.
  */
@@ -287,8 +288,9 @@ int df_kv4_read(const void* cache, void* k, void* v, int B, int L, int kv_heads,
 /*
  * Attention over a 4-bit cache, and to an encoder's states.  out [B, Lq, heads, d] (contiguous) = softmax(q k^T * scale) v per head; heads
  * is a multiple of kv_heads, and heads h of a group share key head h / (heads / kv_heads).  q and other rows: strides as above, in multiples of
- * 16 bytes, rows of k and v at most 2^24 elements apart.  scale positive and below 2.35e38.  A query without any key gives zeros.  bf16 rounds the weights of the keys to bf16 for the matrix
- * instructions; everything else is float.
+ * 16 bytes, rows of k and v at most 2^24 elements apart.  scale positive and below 2.35e38.  A query without any key gives zeros.  bf16 rounds the
+ * weights of the keys to bf16 for the matrix instructions; everything else is float: scores (with the scale) of 2^30 and more in magnitude, and values
+ * whose sum over the keys leaves float's range, give infinities or NaN.  out must not overlap what is read.
  *   df_attn_kv4            all keys from the cache: its L rows, or the first lens[b] of batch item b (device memory, NULL: L; clamped to
  *                          0 .. L; what the other rows hold does not matter).
  *   df_attn_displaced_kv4  df_attn_displaced_axis with the stale rows in a cache: Lq = L / N queries, the patch's own rows from

@@ -54,8 +54,10 @@ __device__ __forceinline__ long long own_row(const Kv4Params& p, int j) {
 
 // A workgroup per tile of 64 keys of a head; D / 8 lanes share a row, eight values each.  The codes of a value's 64 keys lie side by side, so
 // the values' codes cross LDS.  Rows that are not the patch's keep their bytes; a byte that holds one key of the patch and one that is not is
-// read and written by one lane, every other byte is written whole.  Bound by the conversion: a division, a correctly rounded quotient per value; a
-// strip of 31 of 124 columns, 128 rows, 10 heads of 128 (20 MB read): 15.2 us; 300 rows of 20 heads of 64: 3.7 us, the latency of a launch.
+// read and written by one lane, every other byte is written whole.  Bound by the conversion as it is
+// dealt out: each lane of a row divides twice and rounds a quotient per value, and a wave with one row of the patch converts all of its.  A
+// strip of 31 of 124 columns, 128 rows, 10 heads of 128 (20 MB read, about a quarter of the rows its own): 15 - 17 us, where the bytes take 5; 300 rows of
+// 20 heads of 64: 4.4 - 4.8 us, the latency of a launch.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_refresh_kernel(Kv4Params p) {
   constexpr int G = D / 8, ROWS = 256 / G, PASS = 64 / ROWS, PITCH = G + 1;
@@ -140,7 +142,7 @@ __device__ __forceinline__ void turn_values(const unsigned char* vt, unsigned in
   }
 }
 
-// A tile of a head per workgroup; bound by memory: 15872 rows of 10 heads of 128 (21 MB of codes to 81 MB): 15.4 us, 6.6 TB/s
+// A tile of a head per workgroup; bound by memory: 15872 rows of 10 heads of 128 (21 MB of codes to 81 MB): 14.2 - 15.9 us, 6.5 TB/s
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Params p) {
   constexpr int G = D / 8, ROWS = 256 / G, PASS = 64 / ROWS, PITCH = G + 1;
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Params p) {
 }
 
 // The rows that are not the patch's as bf16, side by side per head: what attention with many queries reads (qattn.hip), the conversion
-// once for all blocks of rows.  8400 rows of 10 heads of 64: 7.0 us, 50400: 25.7 (168 MB, 6.5 TB/s)
+// once for all blocks of rows.  8400 rows of 10 heads of 64: 7.8 - 8.5 us, 50400: 26 (168 MB, 6.4 TB/s)
 template <int D>
 __global__ __launch_bounds__(256) void kv4_expand_kernel(Kv4Params p, const int* lens, long long rows) {
   constexpr int G = D / 8, ROWS = 256 / G, PASS = 64 / ROWS, PITCH = G + 1;

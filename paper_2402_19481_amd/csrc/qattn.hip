@@ -7,7 +7,7 @@
 //
 // bf16: S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16 (a lane owns one row of queries; the exponentiated accumulators of S^T are,
 // by the order in which keys are assigned to its rows, the operand P^T without any data movement).  P is rounded to bf16 as the matrix
-// instruction takes it (2^-9 of each weight, averaged over the keys); sums, maxima and O are float, the row sums are those of the float weights.
+// instruction takes it (by 2^-8 of a weight at most, averaged over the keys); sums, maxima and O are float, the row sums are those of the float weights.
 // float: the same on v_mfma_f32_32x32x2_f32, for the small full-precision networks.
 #include <cstring>
 
@@ -107,9 +107,12 @@ __device__ __forceinline__ Share share_of_keys(const QParams& p, Share s, int nr
 // take S_{t+1} as they come free.  K and V tiles go memory -> LDS by direct loads, K_{t+3} and V_{t+1} in iteration t, to rings of four slots (so
 // that K_t is there to the end of iteration t, and all slots follow from one number).  With one wave on a SIMD every instruction takes its time
 // slot, scalar ones too: runs of whole tiles of one segment go through a loop that only moves its pointers on.
-// Bound by instruction issue: of a tile's 1460 cycles (64 values; 215 instructions) the matrix unit works 512, and a second workgroup on the unit adds
-// 16 %.  7200 queries, 10 heads of 64: 5120 keys 124 us (0.76 PFLOP/s), 57600 rows of a cache 1150 (0.92); 16384 queries, 16 heads of 128 on 2048 keys
-// 300 us (0.92), on 512 keys 104 - 110 (8 tiles a block, whose beginning and end take the time of five).
+// Many keys: bound by instruction issue: of a tile's 1460 cycles (64 values; 215 instructions) the matrix unit works 512, and a second workgroup on the
+// unit adds 16 %.  7200 queries, 10 heads of 64: 5120 keys 124 us (0.76 PFLOP/s), 57600 rows of a cache 1065 - 1220 (0.87 - 1.0); 16384 queries, 16 heads
+// of 128 on 2048 keys 300 us (0.92), on 512 keys with a mask 112 - 114 (six or seven tiles a block, whose beginning and end take the time of five).
+// With fewer keys that is not all of it: 1200 queries on 9600 rows, 10 heads of 64, take 49 - 51 us (two workgroups on every unit, equal shares,
+// ending after 30 - 33 and 40 - 44), attn_pipe_d64 on as many rows of bf16 37.  That one has V transposed in memory (8 plain reads of LDS a tile for 16
+// transposing ones, a third of whose cycles are conflicts here) and its queries scaled, which saves 32 of the vector instructions.
 // The running maximum is that of the first tile and moves when a row's weights of a tile sum to more than 2^13 (the sums are needed anyway; the
 // maximum of every tile would be 22 instructions more): by the power of two above the sum, which scales the packed weights exactly, or, beyond 2^100,
 // to the tile's own maximum, with the tile done again from its K in LDS.
@@ -691,7 +694,8 @@ __global__ __launch_bounds__(256) void merge_shares(QParams p, Share planned, in
 // Rows of segment 0 that the mask (and the length) leaves, side by side per head, with zeros behind their d values, and how many they are per batch
 // item: the pipelined loop then has whole tiles of keys, and none for what is masked (its own words and biases per tile cost it 20 us of 150 at 7200
 // queries, 5120 keys, 10 heads of 64, with every key there).  A workgroup copies those of 64 rows of a head; it counts the ones before them itself.
-// Bound by memory: 512 rows of 8 heads of 128 take 6 us (the launch is 3 of them).
+// Bound by memory: 512 rows of 8 heads of 128 take 5.5 us (the launch is 3 of them).  The counting grows with the square of the rows: one query, 100000
+// keys, 8 heads of 64: 146 - 161 us with a mask, 53 without.
 __global__ __launch_bounds__(256) void keep_rows(QParams p, int tiles, bf16_t* ko, bf16_t* vo, int* counts) {
   __shared__ int before[4];
   __shared__ unsigned long long word;
@@ -743,8 +747,8 @@ __global__ __launch_bounds__(256) void keep_rows(QParams p, int tiles, bf16_t* k
 // ---- few keys ----
 // The keys of a split, at most kHeldBytes of them, are brought to LDS once (every load in flight at a time) and stay there; each wave then takes
 // blocks of 32 rows on its own, without barriers.  For short prompts, for patches whose keys are few, and, with the keys split over workgroups, for
-// few rows against more keys.  300 queries, 77 keys, 2 x 20 heads of 64: 5.4 us, of which a launch is 3; 300 queries, 2560 keys, 20 heads: 21 us
-// (pipelined 23).  KV4: segment 0 is the 4-bit cache itself, converted on its way to LDS (levels times scale is exact in bf16), V
+// few rows against more keys.  300 queries, 77 keys, 2 x 20 heads of 64: 5.6 us, of which a launch is 3; 300 queries, 2560 keys, 20 heads: 21 us
+// (pipelined 23); 300 queries beside a cache of 2400 rows, 20 heads: 24 us with the merge (attn_displaced on rows of bf16: 18).  KV4: segment 0 is the 4-bit cache itself, converted on its way to LDS (levels times scale is exact in bf16), V
 // transposed as it is held; the patch's own rows of it are no keys.
 constexpr int kHeldBytes = 128 * 1024;
 __device__ const u32x4 kZeros[1] = {};
@@ -1215,7 +1219,7 @@ __global__ __launch_bounds__(256) void float_attn(QParams p, int kw) {
 // summed; every wave takes every fourth tile.  A lane's dword of codes is eight values of a key (K) or eight keys of a value (V): an operand of
 // v_mfma_f32_16x16x32_bf16 once its levels, which are exact in bf16, are converted.  The scales are those of keys: they multiply the scores and
 // the weights, in float.  Score register (kb, r) of lane group gg is key 16 gg + 4 kb + r.  Bound by memory: one query on 57600 keys, 4 x 20 heads of
-// 64 (313 MB of codes and scales): 59 us, 5.3 TB/s; on 1037 keys, 4 x 5 heads: 5.3 us.
+// 64 (313 MB of codes and scales): 57 - 59 us, 5.4 TB/s; on 1037 keys, 4 x 5 heads: 5.0 - 5.3 us.
 template <int D, int NQ>
 __global__ __launch_bounds__(256, 2) void few_rows_kv4(QParams p) {
   constexpr int KS = D / 32, DB = D / 16, CPL = D / 4;     // k-steps, blocks of 16 values, values of a key per lane

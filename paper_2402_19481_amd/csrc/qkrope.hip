@@ -51,8 +51,8 @@ __device__ __forceinline__ void st_n(bf16_t* p, const float (&v)[4]) {
 
 // G lanes share a head's row, V values each; a wave takes `steps` (at most four) times 64 / G heads of one token, so the token's angles and the scales are
 // read once.  HALVES: value i turns with value i + half, which another lane of the row has normed; else with its neighbour.
-// Bound by memory: 14401 tokens, 20 + 4 heads of 128 in float 61 - 64 us (5.6 TB/s); one token 2.8 us, 2400 tokens of 20 heads of 64 in bf16 by halves
-// 5.7, the latency of one wave's reads and writes.
+// Bound by memory: 14401 tokens, 20 + 4 heads of 128 in float 62 - 65 us (5.6 TB/s); one token 2.8 - 3.2 us, 2400 tokens of 20 heads of 64 in bf16 by
+// halves 5.7 - 6.2, the latency of one wave's reads and writes.
 template <typename T, int V, int G, bool NORM, bool HALVES>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p) {
   constexpr int U = 4;                                     // rows of a lane, at most
