@@ -13,6 +13,14 @@ pytestmark = pytest.mark.gpu
 BF16 = torch.bfloat16
 
 
+@pytest.fixture(autouse=True)
+def _large_blocks_go_back():
+    """(Tests of what happens where memory is short count what torch holds.)"""
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
 def _rows(seed, *shape, std=1.0):
     return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std).to(BF16).to(DEV)
 
